@@ -379,6 +379,166 @@ int moe_layer_fwd(const moe_shape* shape, const moe_layer_options* options, cons
 int moe_layer_bwd(const moe_shape* shape, const moe_layer_options* options, const moe_layer_buffers* buffers,
                   const void* x, const float* Wg, const void* W1, const void* W2, const void* dy, void* stream);
 
+/* ---------------------------------------------------------------------------------
+ * Wide gates: any of 1..8 experts per token, chosen within groups of experts
+ * ---------------------------------------------------------------------------------
+ * A second gate beside moe_gate_route, for layers with many experts.  It chooses and
+ * weights experts; moe_sort_choices then gives every choice a row of its own, expert by
+ * expert, so that there is no capacity and nothing is dropped.
+ * Limits: T >= 1; 1 <= k <= 8; k <= E <= 256; T*k < 2^30; n_groups divides E, and
+ * 1 <= top_groups <= n_groups <= 64; group_best is 1 or 2 and at most E / n_groups;
+ * k <= top_groups * (E / n_groups); scale is finite (else MOE_ERR_SHAPE); an unknown score
+ * is MOE_ERR_DTYPE. */
+enum moe_score { MOE_SOFTMAX = 0, MOE_SIGMOID = 1 };
+
+typedef struct {
+    int32_t T, E, k;
+    int32_t score;       /* moe_score */
+    int32_t n_groups;    /* 1 = no groups */
+    int32_t top_groups;  /* groups that a token may choose from */
+    int32_t group_best;  /* a group counts by its best expert (1), or by its best two (2) */
+    int32_t renormalise; /* divide the weights by the sum of the chosen scores */
+    float scale;         /* factor of every weight */
+} moe_router;
+
+/* Choices and weights.
+ *   s[t,e]          = softmax over e of logits[t,:], or 1 / (1 + exp(-logits[t,e]))
+ *   v[t,e]          = s[t,e] + select_bias[e], in 64 bits; logits[t,e] without a bias
+ *   With n_groups > 1, group g holds the E / n_groups consecutive experts from g * E / n_groups;
+ *   its value is the largest v of its experts, or (group_best 2) the sum of the two largest
+ *   s + select_bias.  Only experts of the top_groups groups of the largest values can be chosen.
+ *   expert_idx[T,k] = the k experts with the largest v, best first
+ *   gate_w[T,k]     = scale * s / (sum of the token's chosen s), or scale * s
+ * Ties go to the smaller id, of groups and of experts.  The bias decides who is chosen and has
+ * no part in the weights.  An expert whose logit is -inf (masked) scores 0 and is chosen only
+ * where its token has no other; a NaN logit counts as -inf in the choice.  A logistic score below
+ * 1e-299 (a logit below -690) counts as 0.  The weights of a token whose chosen scores are all 0 are 0.  Infinite logits and NaN give undefined weights, never an
+ * index out of range.  Tokens with token_mask[t] == 0 (padding) get choices -1 and weights 0, and
+ * their logits are not read. */
+int moe_router_fwd(const moe_router* router, const float* logits, const float* select_bias_or_null,
+                   const uint8_t* token_mask_or_null, int32_t* expert_idx, float* gate_w, void* stream);
+
+/* Derivative of gate_w with respect to the logits; the choice is a constant.  With c = scale,
+ * over the token's choices j (those outside 0..E-1 count for nothing), r = s / (sum of s):
+ *   q_j = c r_j (dgate_w_j - sum_i dgate_w_i r_i), or c s_j dgate_w_j without renormalise
+ *   softmax:  dlogits[t,e] = sum of the q_j with expert_idx[t,j] == e, - s[t,e] * sum_j q_j
+ *   sigmoid:  dlogits[t,e] = sum of the q_j (1 - s_j) with expert_idx[t,j] == e
+ * dlogits[T,E] is overwritten; rows of padding become 0. */
+int moe_router_bwd(const moe_router* router, const float* logits, const int32_t* expert_idx,
+                   const float* dgate_w, float* dlogits, void* stream);
+
+/* Rows of the choices, expert by expert: expert_start[e] = number of choices of experts below
+ * e (expert_start[E] = all of them), and the choices of one expert get the rows from there on in
+ * order of t*k+j: row_of[T,k] in 0 .. expert_start[E]-1.  A choice outside 0..E-1 gets -1.
+ * Needs moe_sort_workspace_bytes() of workspace (0 on an invalid router). */
+size_t moe_sort_workspace_bytes(const moe_router* router);
+int moe_sort_choices(const moe_router* router, const int32_t* expert_idx, int32_t* row_of,
+                     int32_t* expert_start, void* ws, size_t ws_bytes, void* stream);
+
+/* Balance without a loss: select_bias[e] += rate for experts with fewer choices than the mean,
+ * -= rate for those with more (compared exactly, in whole numbers).  expert_start[E+1] as
+ * moe_sort_choices gives it. */
+int moe_router_bias_update(const moe_router* router, const int32_t* expert_start, float rate,
+                           float* select_bias, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * Experts on 8-bit operands (forward only)
+ * ---------------------------------------------------------------------------------
+ * Format.  Values are e4m3 (finite, one NaN), with one power of two for a block of 128:
+ * x ~ q * 2^(b - 127) with the byte b; b - 127 is the smallest exponent e (not below -127) with
+ * max |x| * 2^-e <= 448 over the block, 0 for a block of zeros; q = x * 2^-e rounded to nearest,
+ * ties to even.  With K entries in the reduction, Kp = K rounded up to 128, Kb = Kp / 128 rounded
+ * up to 4:
+ *   rows     q[rows, Kp] and b[rows, Kb]: a block is 128 entries of one row
+ *   weights  q[E, Np, Kp] and b[E, Np/128, Kb], the matrices [K, N] transposed, Np = N rounded up
+ *            to 128: a block is 128 x 128
+ * Entries behind K and N are 0, bytes behind Kp / 128 are 127.  A value that is not finite becomes
+ * NaN, and the finite values of its block are rounded with an exponent of 120 or more.  All
+ * arrays start on 16 bytes.
+ * Rows are grouped by expert as moe_sort_choices does it: expert e has the rows expert_start[e]
+ * .. expert_start[e+1]-1; entries of expert_start outside 0..rows count as the nearest of the two,
+ * and they must not decrease.  Rows behind the last expert's are neither read nor written.
+ * Limits: K, N, d_model, d_ff multiples of 8 from 8 to 2^20; 1 <= E <= 256; rows and T*k < 2^30; one expert's weights
+ * Np * Kp < 2^31 (else MOE_ERR_SHAPE). */
+int moe_quantise_rows_fp8(int32_t rows, int32_t K, int32_t dtype, const void* x, void* q, uint8_t* b,
+                          void* stream);
+/* W[E,K,N] of type dtype */
+int moe_quantise_weights_fp8(int32_t E, int32_t K, int32_t N, int32_t dtype, const void* W, void* q,
+                             uint8_t* b, void* stream);
+
+/* y[r,:] = x[r,:] * W_e for the rows r of every expert e, y[rows,N] in bfloat16.  With E = 1 this is an
+ * ordinary product.  The matrix instructions bring the products of 8 neighbouring reduction entries to the
+ * largest one's exponent, where they keep 13 bits below its leading one, and add such sums in fp32: y is
+ * off by less than 7 * 2^-13 of the largest product of each 8 (about 2^-14 of y for random operands), which
+ * is why results are bfloat16 only. */
+int moe_expert_product_fp8(int32_t rows, int32_t E, int32_t K, int32_t N, const void* xq, const uint8_t* xb,
+                           const int32_t* expert_start, const void* Wq, const uint8_t* Wb, void* y, void* stream);
+
+/* T tokens of k choices: R = T*k rows */
+typedef struct {
+    int32_t T, d_model, d_ff, E, k;
+    int32_t dtype; /* of x, yd and y: MOE_BF16 (else MOE_ERR_DTYPE) */
+    int32_t act;   /* moe_act */
+} moe_fp8_shape;
+
+/* Dispatch into 8-bit rows: row row_of[t,j] of xq[R,Kp(d_model)], xb is x[t,:] in 8 bits, for every j with
+ * row_of[t,j] in 0..R-1. */
+int moe_dispatch_fp8(const moe_fp8_shape* shape, const void* x, const int32_t* row_of, void* xq,
+                     uint8_t* xb, void* stream);
+
+/* The experts' block: h = act(x W1) in 8 bits -> hq[R,Kp(d_ff)], hb;  yd[R,d_model] = h W2.  The hidden
+ * activation is formed in fp32 and rounded once, to the format above. */
+int moe_expert_ffn_fwd_fp8(const moe_fp8_shape* shape, const void* xq, const uint8_t* xb,
+                           const int32_t* expert_start, const void* W1q, const uint8_t* W1b,
+                           const void* W2q, const uint8_t* W2b, void* hq, uint8_t* hb, void* yd,
+                           void* stream);
+
+/* y[t,:] = sum over j with row_of[t,j] in 0..R-1 of gate_w[t,j] * yd[row_of[t,j],:] */
+int moe_combine_rows(const moe_fp8_shape* shape, const void* yd, const int32_t* row_of,
+                     const float* gate_w, void* y, void* stream);
+
+/* One pass of such a layer as one call: gate projection (left out where logits_given),
+ * router, sort, dispatch, experts, mixture.  router and shape must agree in T, E and k
+ * (else MOE_ERR_SHAPE).  Buffers as above; ws of moe_sort_workspace_bytes(). */
+typedef struct {
+    float* logits;          /* [T,E] */
+    int32_t* expert_idx;    /* [T,k] */
+    float* gate_w;          /* [T,k] */
+    int32_t* row_of;        /* [T,k] */
+    int32_t* expert_start;  /* [E+1] */
+    void* xq; uint8_t* xb;
+    void* hq; uint8_t* hb;
+    void *yd, *y;
+    void* ws;
+    size_t ws_bytes;
+} moe_fp8_buffers;
+int moe_layer_fwd_fp8(const moe_fp8_shape* shape, const moe_router* router, int32_t logits_given,
+                      const moe_fp8_buffers* buffers, const void* x, const float* Wg,
+                      const float* select_bias_or_null, const uint8_t* token_mask_or_null,
+                      const void* W1q, const uint8_t* W1b, const void* W2q, const uint8_t* W2b, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * Global norm and clipping of gradients
+ * ---------------------------------------------------------------------------------
+ * Over any number of tensors, of float and bfloat16 in any mixture, of any length and aligned to
+ * their elements only.  The list is host memory and is read during the call.  out may be grad
+ * itself (then the tensor is clipped in place); otherwise no output may overlap an input or
+ * another output.  Sums of squares are held in 64 bits and added in a fixed order.
+ *   norm[0] = sqrt(sum of all squares), a device float (inf where it is beyond float)
+ *   out     = grad * (max_norm / norm) where norm > max_norm, else grad
+ * A norm that is not finite leaves the gradients as they are: the caller sees the norm and skips
+ * the update.  max_norm >= 0 and finite (else MOE_ERR_SHAPE). */
+typedef struct {
+    const void* grad;
+    void* out;              /* not used by moe_grad_norm */
+    int64_t n;              /* elements, >= 0 */
+    int32_t dtype;          /* moe_dtype */
+} moe_grad;
+size_t moe_grad_workspace_bytes(const moe_grad* grads, int32_t count);
+int moe_grad_norm(const moe_grad* grads, int32_t count, float* norm, void* ws, size_t ws_bytes, void* stream);
+int moe_clip_grads(const moe_grad* grads, int32_t count, float max_norm, float* norm, void* ws, size_t ws_bytes,
+                   void* stream);
+
 #ifdef __cplusplus
 }
 #endif

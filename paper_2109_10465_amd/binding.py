@@ -13,6 +13,7 @@ LIB_PATH = os.path.join(_HERE, "libmoe_hip.so")
 
 F32, BF16 = 0, 1
 RELU, GELU = 0, 1
+SOFTMAX, SIGMOID = 0, 1
 
 EXPORTS = [
     "moe_status_string", "moe_capacity", "moe_workspace_bytes", "moe_gate_logits", "moe_gate_route",
@@ -26,6 +27,10 @@ EXPORTS = [
     "moe_gate_logits_token_tiles", "moe_gate_logits_bwd_launches", "moe_gate_logits_bwd_chunks",
     "moe_combine_gate_bwd_launches", "moe_expert_ffn_tiles", "moe_expert_ffn_parts",
     "moe_expert_ffn_direct",
+    "moe_router_fwd", "moe_router_bwd", "moe_sort_workspace_bytes", "moe_sort_choices", "moe_router_bias_update",
+    "moe_quantise_rows_fp8", "moe_quantise_weights_fp8", "moe_expert_product_fp8", "moe_dispatch_fp8",
+    "moe_expert_ffn_fwd_fp8", "moe_combine_rows", "moe_layer_fwd_fp8",
+    "moe_grad_workspace_bytes", "moe_grad_norm", "moe_clip_grads",
 ]
 
 
@@ -44,6 +49,26 @@ class LayerBuffers(ctypes.Structure):
 class LayerOptions(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int32) for n in ("groups", "forward_only", "logits_given")]
                 + [(n, ctypes.c_float) for n in ("aux_coef", "jitter_eps", "drop_p")] + [("seed", ctypes.c_uint64)])
+
+
+class MoeRouter(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in
+                 ("T", "E", "k", "score", "n_groups", "top_groups", "group_best", "renormalise")]
+                + [("scale", ctypes.c_float)])
+
+
+class MoeFp8Shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "d_model", "d_ff", "E", "k", "dtype", "act")]
+
+
+class Fp8Buffers(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in
+                ("logits", "expert_idx", "gate_w", "row_of", "expert_start", "xq", "xb", "hq", "hb", "yd", "y",
+                 "ws")] + [("ws_bytes", ctypes.c_size_t)]
+
+
+class MoeGrad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
 class MoeError(RuntimeError):
@@ -73,7 +98,25 @@ def lib():
         L.moe_workspace_bytes.argtypes = [shp]
         L.moe_gate_route_static_max_bytes.restype = sz
         L.moe_gate_route_static_max_bytes.argtypes = []
+        L.moe_sort_workspace_bytes.restype = sz
+        L.moe_sort_workspace_bytes.argtypes = [ctypes.POINTER(MoeRouter)]
+        L.moe_grad_workspace_bytes.restype = sz
+        L.moe_grad_workspace_bytes.argtypes = [vp, i32]
+        rtr, f8 = ctypes.POINTER(MoeRouter), ctypes.POINTER(MoeFp8Shape)
         sigs = {
+            "moe_router_fwd": [rtr] + [vp] * 6,
+            "moe_router_bwd": [rtr] + [vp] * 5,
+            "moe_sort_choices": [rtr] + [vp] * 4 + [sz, vp],
+            "moe_router_bias_update": [rtr, vp, ctypes.c_float, vp, vp],
+            "moe_quantise_rows_fp8": [i32, i32, i32] + [vp] * 4,
+            "moe_quantise_weights_fp8": [i32] * 4 + [vp] * 4,
+            "moe_expert_product_fp8": [i32] * 4 + [vp] * 7,
+            "moe_dispatch_fp8": [f8] + [vp] * 5,
+            "moe_expert_ffn_fwd_fp8": [f8] + [vp] * 11,
+            "moe_combine_rows": [f8] + [vp] * 5,
+            "moe_layer_fwd_fp8": [f8, rtr, i32, ctypes.POINTER(Fp8Buffers)] + [vp] * 9,
+            "moe_grad_norm": [vp, i32, vp, vp, sz, vp],
+            "moe_clip_grads": [vp, i32, ctypes.c_float, vp, vp, sz, vp],
             "moe_gate_route_static": [shp] + [vp] * 10,
             "moe_gate_logits": [shp] + [vp] * 5,
             "moe_gate_route": [shp] + [vp] * 10 + [sz, vp],
@@ -352,3 +395,129 @@ def moe_gate_logits_bwd(shape, x, Wg, dlogits, dWg, dx_accum, ws, stream=None):
                                      _p(dx_accum), _p(ws),
                                      0 if ws is None else ws.numel() * ws.element_size(),
                                      _stream(stream)), "moe_gate_logits_bwd")
+
+
+# ---- wide gates ---------------------------------------------------------------------
+def make_router(T, E, k, score=SOFTMAX, n_groups=1, top_groups=1, group_best=1, renormalise=True, scale=1.0):
+    return MoeRouter(T, E, k, score, n_groups, top_groups, group_best, bool(renormalise), scale)
+
+
+def moe_router_fwd(router, logits, select_bias, token_mask, expert_idx, gate_w, stream=None):
+    _check(lib().moe_router_fwd(ctypes.byref(router), _p(logits), _p(select_bias), _p(token_mask), _p(expert_idx),
+                                _p(gate_w), _stream(stream)), "moe_router_fwd")
+
+
+def moe_router_bwd(router, logits, expert_idx, dgate_w, dlogits, stream=None):
+    _check(lib().moe_router_bwd(ctypes.byref(router), _p(logits), _p(expert_idx), _p(dgate_w), _p(dlogits),
+                                _stream(stream)), "moe_router_bwd")
+
+
+def moe_sort_workspace_bytes(router):
+    return lib().moe_sort_workspace_bytes(ctypes.byref(router))
+
+
+def moe_sort_choices(router, expert_idx, row_of, expert_start, ws, stream=None):
+    _check(lib().moe_sort_choices(ctypes.byref(router), _p(expert_idx), _p(row_of), _p(expert_start), _p(ws),
+                                  0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
+           "moe_sort_choices")
+
+
+def moe_router_bias_update(router, expert_start, rate, select_bias, stream=None):
+    _check(lib().moe_router_bias_update(ctypes.byref(router), _p(expert_start), float(rate), _p(select_bias),
+                                        _stream(stream)), "moe_router_bias_update")
+
+
+# ---- 8-bit operands -----------------------------------------------------------------
+def fp8_padded(n):
+    """Kp or Np: an extent in whole blocks of 128."""
+    return -(-n // 128) * 128
+
+
+def fp8_scale_bytes(K):
+    """Kb: exponent bytes of a row."""
+    return -(-K // 512) * 4
+
+
+def make_fp8_shape(T, d_model, d_ff, E, k, dtype, act):
+    return MoeFp8Shape(T, d_model, d_ff, E, k, dtype, act)
+
+
+def _dtype_of(t):
+    import torch
+    try:
+        return {torch.float32: F32, torch.bfloat16: BF16}[t.dtype]
+    except KeyError:
+        raise MoeError(f"float32 or bfloat16 expected, not {t.dtype}") from None
+
+
+def moe_quantise_rows_fp8(rows, K, x, q, b, stream=None):
+    _check(lib().moe_quantise_rows_fp8(int(rows), int(K), _dtype_of(x), _p(x), _p(q), _p(b), _stream(stream)),
+           "moe_quantise_rows_fp8")
+
+
+def moe_quantise_weights_fp8(E, K, N, W, q, b, stream=None):
+    _check(lib().moe_quantise_weights_fp8(int(E), int(K), int(N), _dtype_of(W), _p(W), _p(q), _p(b), _stream(stream)),
+           "moe_quantise_weights_fp8")
+
+
+def moe_expert_product_fp8(rows, E, K, N, xq, xb, expert_start, Wq, Wb, y, stream=None):
+    if _dtype_of(y) != BF16:
+        raise MoeError("y must be bfloat16")
+    _check(lib().moe_expert_product_fp8(int(rows), int(E), int(K), int(N), _p(xq), _p(xb), _p(expert_start), _p(Wq), _p(Wb),
+                                        _p(y), _stream(stream)), "moe_expert_product_fp8")
+
+
+def moe_dispatch_fp8(shape, x, row_of, xq, xb, stream=None):
+    _check(lib().moe_dispatch_fp8(ctypes.byref(shape), _p(x), _p(row_of), _p(xq), _p(xb), _stream(stream)),
+           "moe_dispatch_fp8")
+
+
+def moe_expert_ffn_fwd_fp8(shape, xq, xb, expert_start, W1q, W1b, W2q, W2b, hq, hb, yd, stream=None):
+    _check(lib().moe_expert_ffn_fwd_fp8(ctypes.byref(shape), _p(xq), _p(xb), _p(expert_start), _p(W1q), _p(W1b), _p(W2q),
+                                        _p(W2b), _p(hq), _p(hb), _p(yd), _stream(stream)), "moe_expert_ffn_fwd_fp8")
+
+
+def moe_combine_rows(shape, yd, row_of, gate_w, y, stream=None):
+    _check(lib().moe_combine_rows(ctypes.byref(shape), _p(yd), _p(row_of), _p(gate_w), _p(y), _stream(stream)),
+           "moe_combine_rows")
+
+
+def moe_layer_fwd_fp8(shape, router, logits_given, buffers, x, Wg, select_bias, token_mask, W1q, W1b, W2q, W2b, stream=None):
+    _check(lib().moe_layer_fwd_fp8(ctypes.byref(shape), ctypes.byref(router), bool(logits_given), ctypes.byref(buffers),
+                                   _p(x), _p(Wg), _p(select_bias), _p(token_mask), _p(W1q), _p(W1b), _p(W2q), _p(W2b),
+                                   _stream(stream)), "moe_layer_fwd_fp8")
+
+
+# ---- gradients of many tensors -------------------------------------------------------
+class Grads:
+    """The list that moe_grad_norm and moe_clip_grads take: pairs (grad, out) of contiguous tensors of one type and
+    length; out may be grad itself, or None for the norm alone.  Keeps its tensors alive."""
+
+    def __init__(self, pairs):
+        self.pairs = [tuple(p) for p in pairs]
+        self.list = (MoeGrad * max(1, len(self.pairs)))()
+        for m, (g, o) in zip(self.list, self.pairs):
+            for t in (g,) if o is None else (g, o):
+                if not t.is_contiguous():
+                    raise MoeError("gradients must be contiguous")
+                if t.dtype != g.dtype or t.numel() != g.numel():
+                    raise MoeError("a gradient and its output must agree in type and length")
+            m.grad, m.out, m.n, m.dtype = _p(g), _p(o), g.numel(), _dtype_of(g)
+
+
+def make_grads(pairs):
+    return Grads(pairs)
+
+
+def moe_grad_workspace_bytes(grads):
+    return lib().moe_grad_workspace_bytes(grads.list, len(grads.pairs))
+
+
+def moe_grad_norm(grads, norm, ws, stream=None):
+    _check(lib().moe_grad_norm(grads.list, len(grads.pairs), _p(norm), _p(ws),
+                               0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "moe_grad_norm")
+
+
+def moe_clip_grads(grads, max_norm, norm, ws, stream=None):
+    _check(lib().moe_clip_grads(grads.list, len(grads.pairs), float(max_norm), _p(norm), _p(ws),
+                                0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "moe_clip_grads")

@@ -346,3 +346,12 @@ int ffn_bwd_check(const moe_shape* s, const void* dyd, const void* xd, const voi
                   const float* dW2, const void* ws, size_t ws_bytes);
 int gate_logits_bwd_check(const moe_shape* s, const void* x, const float* Wg, const float* dlogits, float eps,
                           const float* dWg, const void* ws, size_t ws_bytes);
+int router_status(const moe_router* r);
+int router_fwd_check(const moe_router* r, const float* logits, const int32_t* expert_idx, const float* gate_w);
+int sort_check(const moe_router* r, const int32_t* expert_idx, const int32_t* row_of, const int32_t* expert_start,
+               const void* ws, size_t ws_bytes);
+int fp8_shape_status(const moe_fp8_shape* s);
+int dispatch_fp8_check(const moe_fp8_shape* s, const void* x, const int32_t* row_of, const void* xq, const uint8_t* xb);
+int ffn_fp8_check(const moe_fp8_shape* s, const void* xq, const uint8_t* xb, const int32_t* expert_start, const void* W1q,
+                  const uint8_t* W1b, const void* W2q, const uint8_t* W2b, const void* hq, const uint8_t* hb, const void* yd);
+int combine_rows_check(const moe_fp8_shape* s, const void* yd, const int32_t* row_of, const float* gate_w, const void* y);

@@ -119,3 +119,86 @@ class MoELayer:
         with torch.cuda.graph(graph):
             self.step(x, Wg, bias, W1, W2, rts_keys, dy, seed=seed)
         return graph
+
+    def clip_gradients(self, max_norm, others=()):
+        """Clips the last backward pass's dWg, dW1 and dW2 together with `others` (gradients of the rest of the model: float32
+        or bfloat16, contiguous) to the global norm max_norm, in place, and returns that norm (a device tensor of one float)."""
+        if self.forward_only:
+            raise B.MoeError("this layer was built forward-only")
+        grads = B.make_grads([(g, g) for g in (self.dWg, self.dW1, self.dW2, *others)])
+        need = B.moe_grad_workspace_bytes(grads)
+        if self._clip is None or self._clip[1].numel() < need:
+            self._clip = (torch.empty(1, dtype=torch.float32, device=self.device),
+                          torch.empty(need, dtype=torch.uint8, device=self.device))
+        norm, ws = self._clip
+        B.moe_clip_grads(grads, max_norm, norm, ws)
+        return norm
+
+    _clip = None        # norm and workspace of clip_gradients
+
+
+class Fp8MoELayer:
+    """Forward-only layer with a wide gate and experts on 8-bit operands: gate projection -> router -> rows expert by
+    expert -> 8-bit dispatch -> experts -> mixture, as one native call.  Nothing is dropped: every choice has a row.
+
+    W1, W2: pairs (q, b) of 8-bit weights and their exponent bytes, as quantise_weights() makes them from W1 [E, d_model, d_ff]
+    and W2 [E, d_ff, d_model]."""
+
+    _NAMES = ("logits", "expert_idx", "gate_w", "row_of", "expert_start", "xq", "xb", "hq", "hb", "yd", "y", "ws")
+
+    def __init__(self, T, d_model, d_ff, E, k, dtype, act, W1, W2, score=B.SOFTMAX, n_groups=1, top_groups=1, group_best=1,
+                 renormalise=True, scale=1.0, device="cuda:0"):
+        if not torch.cuda.is_available():
+            raise B.MoeError("Fp8MoELayer needs a GPU; there is no CPU fallback")
+        B.lib()
+        self.shape = B.make_fp8_shape(T, d_model, d_ff, E, k, dtype, act)
+        self.router = B.make_router(T, E, k, score, n_groups, top_groups, group_best, renormalise, scale)
+        nbytes = B.moe_sort_workspace_bytes(self.router)
+        if nbytes == 0:
+            raise B.MoeError("unsupported router")
+        for (q, b), (K, N) in ((W1, (d_model, d_ff)), (W2, (d_ff, d_model))):
+            want = (E, B.fp8_padded(N), B.fp8_padded(K)), (E, B.fp8_padded(N) // 128, B.fp8_scale_bytes(K))
+            if (tuple(q.shape), tuple(b.shape)) != want or q.element_size() != 1 or b.dtype != torch.uint8:
+                raise B.MoeError(f"8-bit weights of shapes {want} expected, not {tuple(q.shape)}, {tuple(b.shape)}")
+            if not (q.is_contiguous() and b.is_contiguous()):
+                raise B.MoeError("8-bit weights must be contiguous")
+        self.W1, self.W2 = W1, W2
+        self.device = torch.device(device)
+        adt, R = _TORCH_DT[dtype], T * k
+
+        def buf(shape, dt):
+            return torch.empty(shape, dtype=dt, device=self.device)
+
+        u8 = torch.uint8
+        self.logits, self.gate_w = buf((T, E), torch.float32), buf((T, k), torch.float32)
+        self.expert_idx, self.row_of = buf((T, k), torch.int32), buf((T, k), torch.int32)
+        self.expert_start = buf((E + 1,), torch.int32)
+        self.xq, self.xb = buf((R, B.fp8_padded(d_model)), u8), buf((R, B.fp8_scale_bytes(d_model)), u8)
+        self.hq, self.hb = buf((R, B.fp8_padded(d_ff)), u8), buf((R, B.fp8_scale_bytes(d_ff)), u8)
+        self.yd, self.y = buf((R, d_model), adt), buf((T, d_model), adt)
+        self.ws = buf((nbytes,), u8)
+
+    @staticmethod
+    def quantise_weights(W):
+        """W [E, K, N] (float32 or bfloat16, on the GPU) -> (q, b) as the experts take them."""
+        E, K, N = W.shape
+        if not W.is_contiguous():
+            raise B.MoeError("weights must be contiguous")
+        q = torch.empty((E, B.fp8_padded(N), B.fp8_padded(K)), dtype=torch.float8_e4m3fn, device=W.device)
+        b = torch.empty((E, B.fp8_padded(N) // 128, B.fp8_scale_bytes(K)), dtype=torch.uint8, device=W.device)
+        B.moe_quantise_weights_fp8(E, K, N, W, q, b)
+        return q, b
+
+    def forward(self, x, Wg=None, logits=None, select_bias=None, token_mask=None):
+        """x [T, d_model]; Wg [d_model, E] fp32, or logits [T, E] fp32 in its place; select_bias [E] fp32; token_mask [T]
+        uint8, 0 for padding (its rows of y are 0)."""
+        if (Wg is None) == (logits is None):
+            raise B.MoeError("either Wg or logits")
+        ptrs = [(logits if n == "logits" and logits is not None else getattr(self, n)).data_ptr() for n in self._NAMES]
+        B.moe_layer_fwd_fp8(self.shape, self.router, logits is not None, B.Fp8Buffers(*ptrs, self.ws.numel()), x, Wg,
+                            select_bias, token_mask, *self.W1, *self.W2)
+        return self.y
+
+    def update_select_bias(self, select_bias, rate):
+        """After a forward pass: raises the bias of experts with fewer choices than the mean by rate, lowers the others'."""
+        B.moe_router_bias_update(self.router, self.expert_start, rate, select_bias)
