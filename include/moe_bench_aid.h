@@ -50,6 +50,10 @@ int moe_expert_ffn_parts(const moe_shape* shape, int32_t* parts);
  * counts, 0 where workgroups walk the tiles that the counts leave; and how many workgroups there are. */
 int moe_expert_ffn_direct(const moe_shape* shape, int32_t* direct, int32_t* workgroups);
 
+/* Kernels of moe_expert_ffn_fwd_fp8's two products: 0 = tiles of 256 x 256, 1 = of 128 x 128, 2 = of 32 x 32 with a split
+ * reduction (second product only). */
+int moe_fp8_kernels(const moe_fp8_shape* shape, int32_t* first, int32_t* second);
+
 #ifdef __cplusplus
 }
 #endif

@@ -466,18 +466,19 @@ int moe_quantise_rows_fp8(int32_t rows, int32_t K, int32_t dtype, const void* x,
 int moe_quantise_weights_fp8(int32_t E, int32_t K, int32_t N, int32_t dtype, const void* W, void* q,
                              uint8_t* b, void* stream);
 
-/* y[r,:] = x[r,:] * W_e for the rows r of every expert e, y[rows,N] in bfloat16.  With E = 1 this is an
+/* y[r,:] = x[r,:] * W_e for the rows r of every expert e, y[rows,N] of type y_dtype.  With E = 1 this is an
  * ordinary product.  The matrix instructions bring the products of 8 neighbouring reduction entries to the
  * largest one's exponent, where they keep 13 bits below its leading one, and add such sums in fp32: y is
- * off by less than 7 * 2^-13 of the largest product of each 8 (about 2^-14 of y for random operands), which
- * is why results are bfloat16 only. */
+ * off by less than 7 * 2^-13 of the largest product of each 8 (about 2^-14 of y for random operands): float
+ * results are for sums that are formed of them, not for more digits. */
 int moe_expert_product_fp8(int32_t rows, int32_t E, int32_t K, int32_t N, const void* xq, const uint8_t* xb,
-                           const int32_t* expert_start, const void* Wq, const uint8_t* Wb, void* y, void* stream);
+                           const int32_t* expert_start, const void* Wq, const uint8_t* Wb, int32_t y_dtype, void* y,
+                           void* stream);
 
 /* T tokens of k choices: R = T*k rows */
 typedef struct {
     int32_t T, d_model, d_ff, E, k;
-    int32_t dtype; /* of x, yd and y: MOE_BF16 (else MOE_ERR_DTYPE) */
+    int32_t dtype; /* of x and y: MOE_BF16 (else MOE_ERR_DTYPE) */
     int32_t act;   /* moe_act */
 } moe_fp8_shape;
 
@@ -486,15 +487,15 @@ typedef struct {
 int moe_dispatch_fp8(const moe_fp8_shape* shape, const void* x, const int32_t* row_of, void* xq,
                      uint8_t* xb, void* stream);
 
-/* The experts' block: h = act(x W1) in 8 bits -> hq[R,Kp(d_ff)], hb;  yd[R,d_model] = h W2.  The hidden
- * activation is formed in fp32 and rounded once, to the format above. */
+/* The experts' block: h = act(x W1) in 8 bits -> hq[R,Kp(d_ff)], hb;  yd[R,d_model] = h W2, of type
+ * yd_dtype.  The hidden activation is formed in fp32 and rounded once, to the format above. */
 int moe_expert_ffn_fwd_fp8(const moe_fp8_shape* shape, const void* xq, const uint8_t* xb,
                            const int32_t* expert_start, const void* W1q, const uint8_t* W1b,
-                           const void* W2q, const uint8_t* W2b, void* hq, uint8_t* hb, void* yd,
-                           void* stream);
+                           const void* W2q, const uint8_t* W2b, void* hq, uint8_t* hb, int32_t yd_dtype,
+                           void* yd, void* stream);
 
 /* y[t,:] = sum over j with row_of[t,j] in 0..R-1 of gate_w[t,j] * yd[row_of[t,j],:] */
-int moe_combine_rows(const moe_fp8_shape* shape, const void* yd, const int32_t* row_of,
+int moe_combine_rows(const moe_fp8_shape* shape, int32_t yd_dtype, const void* yd, const int32_t* row_of,
                      const float* gate_w, void* y, void* stream);
 
 /* One pass of such a layer as one call: gate projection (left out where logits_given),
@@ -508,7 +509,8 @@ typedef struct {
     int32_t* expert_start;  /* [E+1] */
     void* xq; uint8_t* xb;
     void* hq; uint8_t* hb;
-    void *yd, *y;
+    float* yd;              /* float: rows are not rounded before they are summed */
+    void* y;
     void* ws;
     size_t ws_bytes;
 } moe_fp8_buffers;

@@ -29,7 +29,7 @@ EXPORTS = [
     "moe_expert_ffn_direct",
     "moe_router_fwd", "moe_router_bwd", "moe_sort_workspace_bytes", "moe_sort_choices", "moe_router_bias_update",
     "moe_quantise_rows_fp8", "moe_quantise_weights_fp8", "moe_expert_product_fp8", "moe_dispatch_fp8",
-    "moe_expert_ffn_fwd_fp8", "moe_combine_rows", "moe_layer_fwd_fp8",
+    "moe_expert_ffn_fwd_fp8", "moe_combine_rows", "moe_layer_fwd_fp8", "moe_fp8_kernels",
     "moe_grad_workspace_bytes", "moe_grad_norm", "moe_clip_grads",
 ]
 
@@ -110,11 +110,12 @@ def lib():
             "moe_router_bias_update": [rtr, vp, ctypes.c_float, vp, vp],
             "moe_quantise_rows_fp8": [i32, i32, i32] + [vp] * 4,
             "moe_quantise_weights_fp8": [i32] * 4 + [vp] * 4,
-            "moe_expert_product_fp8": [i32] * 4 + [vp] * 7,
+            "moe_expert_product_fp8": [i32] * 4 + [vp] * 5 + [i32, vp, vp],
             "moe_dispatch_fp8": [f8] + [vp] * 5,
-            "moe_expert_ffn_fwd_fp8": [f8] + [vp] * 11,
-            "moe_combine_rows": [f8] + [vp] * 5,
+            "moe_expert_ffn_fwd_fp8": [f8] + [vp] * 9 + [i32, vp, vp],
+            "moe_combine_rows": [f8, i32] + [vp] * 5,
             "moe_layer_fwd_fp8": [f8, rtr, i32, ctypes.POINTER(Fp8Buffers)] + [vp] * 9,
+            "moe_fp8_kernels": [f8, vp, vp],
             "moe_grad_norm": [vp, i32, vp, vp, sz, vp],
             "moe_clip_grads": [vp, i32, ctypes.c_float, vp, vp, sz, vp],
             "moe_gate_route_static": [shp] + [vp] * 10,
@@ -461,10 +462,8 @@ def moe_quantise_weights_fp8(E, K, N, W, q, b, stream=None):
 
 
 def moe_expert_product_fp8(rows, E, K, N, xq, xb, expert_start, Wq, Wb, y, stream=None):
-    if _dtype_of(y) != BF16:
-        raise MoeError("y must be bfloat16")
     _check(lib().moe_expert_product_fp8(int(rows), int(E), int(K), int(N), _p(xq), _p(xb), _p(expert_start), _p(Wq), _p(Wb),
-                                        _p(y), _stream(stream)), "moe_expert_product_fp8")
+                                        _dtype_of(y), _p(y), _stream(stream)), "moe_expert_product_fp8")
 
 
 def moe_dispatch_fp8(shape, x, row_of, xq, xb, stream=None):
@@ -474,11 +473,12 @@ def moe_dispatch_fp8(shape, x, row_of, xq, xb, stream=None):
 
 def moe_expert_ffn_fwd_fp8(shape, xq, xb, expert_start, W1q, W1b, W2q, W2b, hq, hb, yd, stream=None):
     _check(lib().moe_expert_ffn_fwd_fp8(ctypes.byref(shape), _p(xq), _p(xb), _p(expert_start), _p(W1q), _p(W1b), _p(W2q),
-                                        _p(W2b), _p(hq), _p(hb), _p(yd), _stream(stream)), "moe_expert_ffn_fwd_fp8")
+                                        _p(W2b), _p(hq), _p(hb), _dtype_of(yd), _p(yd), _stream(stream)),
+           "moe_expert_ffn_fwd_fp8")
 
 
 def moe_combine_rows(shape, yd, row_of, gate_w, y, stream=None):
-    _check(lib().moe_combine_rows(ctypes.byref(shape), _p(yd), _p(row_of), _p(gate_w), _p(y), _stream(stream)),
+    _check(lib().moe_combine_rows(ctypes.byref(shape), _dtype_of(yd), _p(yd), _p(row_of), _p(gate_w), _p(y), _stream(stream)),
            "moe_combine_rows")
 
 
@@ -486,6 +486,13 @@ def moe_layer_fwd_fp8(shape, router, logits_given, buffers, x, Wg, select_bias, 
     _check(lib().moe_layer_fwd_fp8(ctypes.byref(shape), ctypes.byref(router), bool(logits_given), ctypes.byref(buffers),
                                    _p(x), _p(Wg), _p(select_bias), _p(token_mask), _p(W1q), _p(W1b), _p(W2q), _p(W2b),
                                    _stream(stream)), "moe_layer_fwd_fp8")
+
+
+def moe_fp8_kernels(shape):
+    """(first, second): 0 = tiles of 256 x 256, 1 = of 128 x 128, 2 = of 32 x 32 with a split reduction."""
+    first, second = ctypes.c_int32(), ctypes.c_int32()
+    _check(lib().moe_fp8_kernels(ctypes.byref(shape), ctypes.byref(first), ctypes.byref(second)), "moe_fp8_kernels")
+    return first.value, second.value
 
 
 # ---- gradients of many tensors -------------------------------------------------------

@@ -21,33 +21,33 @@ struct Fp8Args {
     int xb_stride, yb_stride;       // exponent bytes per row (xb_stride: also per block row of the weights)
 };
 
-enum { OUT_BF16 = 0, OUT_RELU8 = 1, OUT_GELU8 = 2 };
+enum { OUT_BF16 = 0, OUT_F32 = 1, OUT_RELU8 = 2, OUT_GELU8 = 3 };
 
 // one step of 64 reduction entries with the exponents of byte S of either word
 template <int S> __device__ __forceinline__ f32x16_t mma(i32x8_t w, i32x8_t x, f32x16_t c, int we, int xe) {
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, c, 0, 0, S, we, S, xe);
 }
+__device__ __forceinline__ i32x8_t two16(u32x4_buf_t a, u32x4_buf_t b) {
+    return i32x8_t{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+}
 __device__ __forceinline__ i32x8_t two16(uint4 a, uint4 b) {
     return i32x8_t{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
 }
 
-// gelu(z) = z Phi(z), as the fp32 experts have it: two fits of Phi that meet at |z| = 1.0625
+// gelu(z) = z Phi(z) with Phi(z) = 1 / (1 + 2^(-z P(z^2))): the logit of Phi is odd and smooth, and six coefficients of P,
+// fitted to 64 bits on |z| <= 5.5 with equal errors of gelu, leave 1.1e-6 of it (in fp32, over |z| <= 12).  A product
+// wide of the rounding to 8 bits, but an error e of a value moves a share e / step of the roundings, and their effect
+// on the output goes with the root of that: 1e-5 would be seen beside bfloat16's rounding.  18 instruction slots
+// (exponential and reciprocal four each) instead of the 33 of the two fits that the fp32 experts use: the epilogue of
+// the first product is bound by vector instructions.
 __device__ __forceinline__ float gelu(float z) {
-    constexpr float CENTRE[6] = {0.39894229f, -0.066490486f, 0.0099737411f, -0.0011868734f, 0.00011374246f, -7.6692668e-06f};
-    constexpr float MILLS_NUM[4] = {1.2527357f, 1.0029950f, 0.36051896f, 0.061547495f};
-    constexpr float MILLS_DEN[5] = {1.0f, 1.5959138f, 1.0661000f, 0.36044064f, 0.061549164f};
-    constexpr float LH = -0.72134751f, PHI0 = 0.39894228f, PHI0_LN2 = 0.27652571f;
-    const float t = fminf(fabsf(z), 16.0f), s = t * t, e = s * LH, rest = fmaf(s, LH, -e);
-    const float pdf = __builtin_amdgcn_exp2f(e) * fmaf(rest, PHI0_LN2, PHI0);
-    float c = CENTRE[5], num = MILLS_NUM[3], den = MILLS_DEN[4];
+    constexpr float P[6] = {2.3021745681762695f, 0.10492697358131409f, -0.00016549293650314212f, -0.00013676212984137237f,
+                            8.115114724205341e-06f, -1.6478260533858702e-07f};
+    const float s = fminf(z * z, 30.25f);
+    float c = P[5];
 #pragma unroll
-    for (int i = 4; i >= 0; --i) c = fmaf(c, s, CENTRE[i]);
-#pragma unroll
-    for (int i = 2; i >= 0; --i) num = fmaf(num, t, MILLS_NUM[i]);
-#pragma unroll
-    for (int i = 3; i >= 0; --i) den = fmaf(den, t, MILLS_DEN[i]);
-    const float q = num * pdf * __builtin_amdgcn_rcpf(den);
-    return z * (t < 1.0625f ? fmaf(z, c, 0.5f) : (z >= 0.0f ? 1.0f - q : q));
+    for (int i = 4; i >= 0; --i) c = fmaf(c, s, P[i]);
+    return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-z * c));
 }
 
 // lanes 0..31 end with a = (own a, partner's a), lanes 32..63 with (partner's b, own b)
@@ -57,59 +57,76 @@ __device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
     b = r[1];
 }
 
-// The wave's tile of 128 columns (block nb) and 32 rows: acc[f][4 q + i] is column 32 f + 8 q + 4 half + i of row r
+// Values of one matrix tile (columns 32 f + 8 q + 4 half + i of the block nb in v[4 q + i]) of row r: the activation and its
+// largest magnitude so far, and the tile in the output's type.
 template <int OUT>
-__device__ __forceinline__ void store_tile(const Fp8Args& p, f32x16_t (&acc)[4], int nb, int r, bool live, int half) {
+__device__ __forceinline__ float activate(f32x16_t& v, float top) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float z = v[i], h = OUT == OUT_GELU8 ? gelu(z) : (z <= 0.0f ? 0.0f : z);
+        v[i] = h;
+        top = fmaxf(top, fabsf(h));         // (NaN are passed over: they become NaN, whatever the exponent)
+    }
+    return top;
+}
+// g: the reciprocal of the block's unit (8-bit output)
+template <int OUT>
+__device__ __forceinline__ void store_tile(const Fp8Args& p, const f32x16_t& v, int nb, int f, int r, bool live, int half, float g) {
     if constexpr (OUT == OUT_RELU8 || OUT == OUT_GELU8) {
-        uint32_t top = 0;
+        uint32_t d[4];
 #pragma unroll
-        for (int f = 0; f < 4; ++f)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float z = acc[f][i], h = OUT == OUT_GELU8 ? gelu(z) : (z > 0.0f || z != z ? z : 0.0f);
-                acc[f][i] = h;
-                top = max(top, __float_as_uint(h) & 0x7fffffffu);
-            }
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32, MOE_WAVE));
-        const int byte = scale_byte(top);
-        const float g = scale_inverse(byte);
-        uint8_t* row = (uint8_t*)p.y + ((size_t)r * p.nnb + nb) * 128;
-#pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            uint32_t d[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                int w = __builtin_amdgcn_cvt_pk_fp8_f32(acc[f][4 * q] * g, acc[f][4 * q + 1] * g, 0, false);
-                d[q] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(acc[f][4 * q + 2] * g, acc[f][4 * q + 3] * g, w, true);
-            }
-            swap_halves(d[0], d[2]);
-            swap_halves(d[1], d[3]);
-            if (live) *reinterpret_cast<uint4*>(row + 32 * f + 16 * half) = make_uint4(d[0], d[2], d[1], d[3]);
+        for (int q = 0; q < 4; ++q) {
+            const int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * q] * g, v[4 * q + 1] * g, 0, false);
+            d[q] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * q + 2] * g, v[4 * q + 3] * g, w, true);
         }
-        if (live) {
-            uint8_t* bt = p.yb + (size_t)r * p.yb_stride;
-            if (half == 0) bt[nb] = (uint8_t)byte;
-            else if (nb == p.nnb - 1)
-                for (int i = p.nnb; i < p.yb_stride; ++i) bt[i] = 127;
+        swap_halves(d[0], d[2]);
+        swap_halves(d[1], d[3]);
+        if (live)
+            *reinterpret_cast<uint4*>((uint8_t*)p.y + ((size_t)r * p.nnb + nb) * 128 + 32 * f + 16 * half) = make_uint4(d[0], d[2], d[1], d[3]);
+    } else if constexpr (OUT == OUT_F32) {
+        float* row = (float*)p.y + (size_t)r * p.N;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int n = nb * 128 + 32 * f + 8 * q + 4 * half;
+            if (live && n < p.N) *reinterpret_cast<float4*>(row + n) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
         }
     } else {
         bf16_t* row = (bf16_t*)p.y + (size_t)r * p.N;
+        uint32_t d[4][2];
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            uint32_t d[4][2];
+        for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int i = 0; i < 2; ++i) d[q][i] = pack_bf16x2(v[4 * q + 2 * i], v[4 * q + 2 * i + 1]);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) d[q][i] = pack_bf16x2(acc[f][4 * q + 2 * i], acc[f][4 * q + 2 * i + 1]);
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                swap_halves(d[q][0], d[q + 2][0]);
-                swap_halves(d[q][1], d[q + 2][1]);
-                const int n = nb * 128 + 32 * f + 16 * half + 8 * q;
-                if (live && n < p.N) *reinterpret_cast<uint4*>(row + n) = make_uint4(d[q][0], d[q][1], d[q + 2][0], d[q + 2][1]);
-            }
+        for (int q = 0; q < 2; ++q) {
+            swap_halves(d[q][0], d[q + 2][0]);
+            swap_halves(d[q][1], d[q + 2][1]);
+            const int n = nb * 128 + 32 * f + 16 * half + 8 * q;
+            if (live && n < p.N) *reinterpret_cast<uint4*>(row + n) = make_uint4(d[q][0], d[q][1], d[q + 2][0], d[q + 2][1]);
         }
     }
+}
+// the exponent byte of block nb of row r, and behind the last block the bytes that fill up
+__device__ __forceinline__ void store_byte(const Fp8Args& p, int byte, int nb, int r, int half) {
+    uint8_t* bt = p.yb + (size_t)r * p.yb_stride;
+    if (half == 0) bt[nb] = (uint8_t)byte;
+    else if (nb == p.nnb - 1)
+        for (int i = p.nnb; i < p.yb_stride; ++i) bt[i] = 127;
+}
+// all four tiles of a block in one wave
+template <int OUT>
+__device__ __forceinline__ void store_block(const Fp8Args& p, f32x16_t (&acc)[4], int nb, int r, bool live, int half) {
+    float g = 0.0f;
+    if constexpr (OUT == OUT_RELU8 || OUT == OUT_GELU8) {
+        float top = 0.0f;
+#pragma unroll
+        for (int f = 0; f < 4; ++f) top = activate<OUT>(acc[f], top);
+        const int byte = scale_byte(__float_as_uint(fmaxf(top, __shfl_xor(top, 32, MOE_WAVE))));
+        g = scale_inverse(byte);
+        if (live) store_byte(p, byte, nb, r, half);
+    }
+#pragma unroll
+    for (int f = 0; f < 4; ++f) store_tile<OUT>(p, acc[f], nb, f, r, live, half, g);
 }
 
 // Which expert and rows the row tile `at` has, tiles of TR rows, expert by expert: found by a wave, four experts a lane
@@ -143,51 +160,352 @@ __device__ __forceinline__ RowTile find_tile(const int32_t* __restrict__ start, 
     return {__shfl(r.e, src, MOE_WAVE), __shfl(r.row, src, MOE_WAVE), __shfl(r.end, src, MOE_WAVE)};
 }
 
-// one wave: 128 columns and 32 rows, operands straight from memory
+// ---------------------------------------------------------------------------
+// few rows and few columns: a product whose tiles would leave most of the chip idle (the second product of a token or two)
+// ---------------------------------------------------------------------------
+// A workgroup has 32 columns and 32 rows; its eight waves take an eighth of the reduction each, with the operands
+// straight from memory in registers, four blocks of 128 on their way at a time, and nothing shared before the
+// partial sums meet in LDS.
+#define THIN8_WAVES 8
+struct Fp8Slab {            // 128 reduction entries
+    u32x4_buf_t w[4], x[4];         // 16-byte chunks 2 j + half
+    int we, xe;
+};
+
 template <int OUT>
-__global__ __launch_bounds__(64) void fp8_gemm_kernel(const Fp8Args p) {
-    const int lane = threadIdx.x, l32 = lane & 31, half = lane >> 5, nb = blockIdx.x % p.nnb;
-    const RowTile t = find_tile<32>(p.start, p.E, p.rows, blockIdx.x / p.nnb, lane);
+__global__ __launch_bounds__(64 * THIN8_WAVES, 2) void fp8_thin_kernel(const Fp8Args p) {
+    static_assert(OUT == OUT_BF16 || OUT == OUT_F32, "a block's largest magnitude would need four such tiles");
+    __shared__ float4 s_part[THIN8_WAVES][4][64];       // [wave][q][lane]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, half = lane >> 5, ct = blockIdx.x % (4 * p.nnb), nb = ct >> 2;
+    const RowTile t = find_tile<32>(p.start, p.E, p.rows, blockIdx.x / (4 * p.nnb), lane);
     if (t.e < 0) return;
-    const int r = t.row + l32;
-    const bool live = r < t.end;
-    const size_t kbytes = (size_t)p.nkb * 128;
-    const uint8_t* x = p.xq + (size_t)(live ? r : t.row) * kbytes + 16 * half;
-    const uint8_t* w = p.wq + ((size_t)t.e * p.nnb + nb) * 128 * kbytes + (size_t)l32 * kbytes + 16 * half;
-    const int* xe = reinterpret_cast<const int*>(p.xb + (size_t)(live ? r : t.row) * p.xb_stride);
-    const int* we = reinterpret_cast<const int*>(p.wb + ((size_t)t.e * p.nnb + nb) * p.xb_stride);
-    f32x16_t acc[4];
+    // rows behind the expert's last one, and entries behind the wave's part, are beyond the buffers: zeros
+    const uint32_t kbytes = (uint32_t)p.nkb * 128;
+    const size_t left = t.end - t.row;
+    const auto wr = buf_rsrc(p.wq + (((size_t)t.e * p.nnb + nb) * 128 + 32 * (ct & 3)) * kbytes, (size_t)32 * kbytes);
+    const auto xr = buf_rsrc(p.xq + (size_t)t.row * kbytes, left * kbytes);
+    const auto wer = buf_rsrc(p.wb + ((size_t)t.e * p.nnb + nb) * p.xb_stride, p.xb_stride);
+    const auto xer = buf_rsrc(p.xb + (size_t)t.row * p.xb_stride, left * p.xb_stride);
+    const uint32_t off = l32 * kbytes + 16 * half, xoff = l32 * p.xb_stride;
+    f32x16_t acc;
 #pragma unroll
-    for (int f = 0; f < 4; ++f)
+    for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
+    const int per = (p.nkb + THIN8_WAVES - 1) / THIN8_WAVES, k0 = wave * per, k1 = min(k0 + per, p.nkb);
+    auto load = [&](Fp8Slab& s, int kb) {
+        const bool in = kb < k1;
+        const uint32_t o = in ? off + kb * 128 : BUF_OOB;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[f][i] = 0.0f;
-    auto block = [&](int kb, auto byte, int we4, int xe4) {
+        for (int j = 0; j < 4; ++j) {
+            s.w[j] = __builtin_amdgcn_raw_buffer_load_b128(wr, o + 32 * j, 0, 0);
+            s.x[j] = __builtin_amdgcn_raw_buffer_load_b128(xr, o + 32 * j, 0, 0);
+        }
+        s.we = __builtin_amdgcn_raw_buffer_load_b8(wer, in ? kb : BUF_OOB, 0, 0);
+        s.xe = __builtin_amdgcn_raw_buffer_load_b8(xer, in ? xoff + kb : BUF_OOB, 0, 0);
+    };
+    Fp8Slab s[4];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const size_t at = (size_t)kb * 128 + 64 * s;
-            const i32x8_t b = two16(*reinterpret_cast<const uint4*>(x + at), *reinterpret_cast<const uint4*>(x + at + 32));
+    for (int i = 0; i < 4; ++i) load(s[i], k0 + i);
+    __builtin_amdgcn_sched_barrier(0);
+    for (int kb = k0; kb < k1; kb += 4) {
 #pragma unroll
-            for (int f = 0; f < 4; ++f) {
-                const uint8_t* wf = w + (size_t)(32 * f) * kbytes + at;
-                const i32x8_t a = two16(*reinterpret_cast<const uint4*>(wf), *reinterpret_cast<const uint4*>(wf + 32));
-                acc[f] = mma<decltype(byte)::value>(a, b, acc[f], we4, xe4);
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                acc = mma<0>(two16(s[i].w[2 * h], s[i].w[2 * h + 1]), two16(s[i].x[2 * h], s[i].x[2 * h + 1]), acc, s[i].we, s[i].xe);
+            load(s[i], kb + 4 + i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) s_part[wave][q][lane] = make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
+    __syncthreads();
+    if (wave >= 4) return;
+    // wave q finishes columns 8 q + 4 half .. +3 of the tile; the sums are added in the waves' order
+    float4 v = s_part[0][wave][lane];
+#pragma unroll
+    for (int u = 1; u < THIN8_WAVES; ++u) {
+        const float4 o = s_part[u][wave][lane];
+        v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+    }
+    const int r = t.row + l32, n = 32 * ct + 8 * wave + 4 * half;
+    if (r >= t.end || n >= p.N) return;
+    if constexpr (OUT == OUT_F32) *reinterpret_cast<float4*>((float*)p.y + (size_t)r * p.N + n) = v;
+    else *reinterpret_cast<uint2*>((bf16_t*)p.y + (size_t)r * p.N + n) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+}
+
+// ---------------------------------------------------------------------------
+// tiles staged through LDS
+// ---------------------------------------------------------------------------
+// WF x WT waves; a wave has 128 columns and 32 TT rows, four by TT matrix tiles of 32 x 32.  A slab is 128 reduction
+// entries of the tile's columns and rows; two slabs are in LDS, the next one being filled by loads that write LDS
+// themselves.  A workgroup walks its tiles and treats their slabs as one stream, so the next tile's first slab is on
+// its way during a tile's epilogue.
+template <int WF, int WT, int TT>
+struct Fp8Tile {
+    static constexpr int NW = WF * WT, NT = 64 * NW;
+    static constexpr int BF = 128 * WF, BT = 32 * TT * WT;          // columns and rows
+    static constexpr int STAGE = (BF + BT) * 128;
+    static constexpr int WL = BF / 8 / NW, XL = BT / 8 / NW;        // loads of a slab per wave: 8 rows of 128 bytes each
+    static constexpr int TABLE = 2 * STAGE;                         // running tile counts and starts behind the stages
+    static constexpr int BYTES = TABLE + (260 + 260) * 4;
+    static_assert(BF % (8 * NW) == 0 && BT % (8 * NW) == 0 && NW % 2 == 0, "whole loads per wave");
+};
+
+#define FP8_BAND 4      // row tiles per band of the walk inside an expert: an XCD's workgroups share 4 row panels at a time
+
+struct Fp8Place { int e, row, end, col; };      // a tile: expert, first row, the expert's end, first block of 128 columns
+
+// which tile is number `at` (found by the whole wave)
+template <int BT, int WF>
+__device__ __forceinline__ Fp8Place fp8_place(const int* tiles, const int* start, int at, int ctiles, int lane) {
+    const int4 t = *reinterpret_cast<const int4*>(tiles + 4 * lane);        // running counts in front of four experts
+    const int next = tiles[4 * lane + 4];
+    int q = -1;
+    if (at >= t.x && at < t.y) q = 0;
+    else if (at >= t.y && at < t.z) q = 1;
+    else if (at >= t.z && at < t.w) q = 2;
+    else if (at >= t.w && at < next) q = 3;
+    const int src = __ffsll((long long)__ballot(q >= 0)) - 1;
+    const int e = __builtin_amdgcn_readfirstlane(__shfl(4 * lane + q, src, MOE_WAVE));
+    const int in = at - __builtin_amdgcn_readfirstlane(tiles[e]);
+    const int s0 = __builtin_amdgcn_readfirstlane(start[e]), s1 = __builtin_amdgcn_readfirstlane(start[e + 1]);
+    const int rt = (s1 - s0 + BT - 1) / BT, band = in / (FP8_BAND * ctiles), high = min(FP8_BAND, rt - FP8_BAND * band);
+    const int within = in - band * FP8_BAND * ctiles, col = within / high;
+    return {e, __builtin_amdgcn_readfirstlane(s0 + (FP8_BAND * band + within - col * high) * BT), s1,
+            __builtin_amdgcn_readfirstlane(col * WF)};
+}
+
+template <int WF, int WT, int TT, int OUT>
+__global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args p) {
+    typedef Fp8Tile<WF, WT, TT> G;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    int* tiles = reinterpret_cast<int*>(smem + G::TABLE);
+    int* start = tiles + 260;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, half = lane >> 5, wf = wave / WT, wt = wave % WT;
+    const int ctiles = (p.nnb + WF - 1) / WF;
+    if (wave == 0) {
+        int s[5], t[4], n = 0;
+#pragma unroll
+        for (int q = 0; q < 5; ++q) s[q] = min(max(p.start[min(4 * lane + q, p.E)], 0), p.rows);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            t[q] = 4 * lane + q < p.E ? (max(s[q + 1] - s[q], 0) + G::BT - 1) / G::BT * ctiles : 0;
+            n += t[q];
+        }
+        int run = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int u = __shfl_up(run, o, MOE_WAVE);
+            if (lane >= o) run += u;
+        }
+        if (lane == 63) { tiles[256] = run; start[256] = s[4]; }
+        run -= n;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            tiles[4 * lane + q] = run;
+            start[4 * lane + q] = s[q];
+            run += t[q];
+        }
+    }
+    __syncthreads();
+    const int total = __builtin_amdgcn_readfirstlane(tiles[256]);
+    // workgroup w is on XCD w % 8; an XCD takes as many consecutive tiles at a time as it has workgroups
+    const int per = gridDim.x >> 3, xcd = blockIdx.x & 7;
+    int at = xcd * per + (blockIdx.x >> 3);
+    if (at >= total) return;
+    const int stride = per * 8;
+    const uint32_t kbytes = (uint32_t)p.nkb * 128;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)smem;
+
+    // loads of a slab: lane l fills 16 bytes of row 8 m + l / 8; the chunks of a row are permuted by bits 1..3 of the row, so
+    // that 16 rows' reads of one chunk hit all 64 banks
+    const int lrow = lane >> 3, chunk = (lane & 7) ^ (((lrow >> 1) + 4 * (wave & 1)) & 7);
+    uint32_t voff[G::WL > G::XL ? G::WL : G::XL];
+#pragma unroll
+    for (int i = 0; i < (G::WL > G::XL ? G::WL : G::XL); ++i)
+        voff[i] = (uint32_t)((i * G::NW + wave) * 8 + lrow) * kbytes + 16 * chunk;
+    // fragment reads
+    uint32_t frag[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) frag[c] = l32 * 128 + (((4 * (c >> 1) + 2 * half + (c & 1)) ^ ((l32 >> 1) & 7)) << 4);
+    const uint32_t wbase = wf * 128 * 128, xbase = G::BF * 128 + wt * TT * 32 * 128;
+
+    // the cursor of the loads, one slab ahead of the products
+    Fp8Place next = fp8_place<G::BT, WF>(tiles, start, at, ctiles, lane);
+    int nkb = 0;                        // its slab
+    bool more = true;
+    u32x4_buf_t wd, xd;
+    int we_next = 0, xe_next[TT];
+    auto scalar = [](u32x4_buf_t d) {       // (the compiler does not see that a whole wave has the same ones)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)d[i]);
+        return d;
+    };
+    auto aim = [&]() {
+        const uint32_t wleft = (uint32_t)(p.nnb - next.col) * 128 * kbytes;
+        wd = make_desc(p.wq + ((size_t)next.e * p.nnb + next.col) * 128 * kbytes, wleft);
+        const size_t xleft = (size_t)(next.end - next.row) * kbytes;
+        xd = make_desc(p.xq + (size_t)next.row * kbytes, xleft < 0x7fffffffull ? (uint32_t)xleft : 0x7fffffffu);
+    };
+    auto fetch = [&](int stage) {
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + stage * G::STAGE);
+        const u32x4_buf_t wdesc = scalar(wd), xdesc = scalar(xd);
+        if ((nkb & 3) == 0) {
+            const int nb = min(next.col + wf, p.nnb - 1);
+            we_next = *reinterpret_cast<const int*>(p.wb + ((size_t)next.e * p.nnb + nb) * p.xb_stride + nkb);
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                const int r = min(next.row + (wt * TT + t) * 32 + l32, next.end - 1);
+                xe_next[t] = *reinterpret_cast<const int*>(p.xb + (size_t)r * p.xb_stride + nkb);
             }
         }
+#pragma unroll
+        for (int i = 0; i < G::WL; ++i) load_to_lds(wdesc, voff[i], to + (i * G::NW + wave) * 1024);
+#pragma unroll
+        for (int i = 0; i < G::XL; ++i) load_to_lds(xdesc, voff[i], to + G::BF * 128 + (i * G::NW + wave) * 1024);
+        if (++nkb == p.nkb) {
+            nkb = 0;
+            at += stride;
+            more = at < total;
+            if (more) {
+                next = fp8_place<G::BT, WF>(tiles, start, at, ctiles, lane);
+                aim();
+            }
+        } else {
+            // the next slab: 128 bytes further, and as much less to the end
+            uint64_t a = ((uint64_t)wd[1] << 32 | wd[0]) + 128;
+            wd[0] = (uint32_t)a; wd[1] = (uint32_t)(a >> 32); wd[2] = wd[2] > 128 ? wd[2] - 128 : 0;
+            a = ((uint64_t)xd[1] << 32 | xd[0]) + 128;
+            xd[0] = (uint32_t)a; xd[1] = (uint32_t)(a >> 32); xd[2] = xd[2] > 128 ? xd[2] - 128 : 0;
+        }
     };
-    for (int kb = 0; kb < p.nkb; kb += 4) {
-        const int we4 = we[kb >> 2], xe4 = xe[kb >> 2];
-        block(kb, std::integral_constant<int, 0>(), we4, xe4);
-        if (kb + 1 < p.nkb) block(kb + 1, std::integral_constant<int, 1>(), we4, xe4);
-        if (kb + 2 < p.nkb) block(kb + 2, std::integral_constant<int, 2>(), we4, xe4);
-        if (kb + 3 < p.nkb) block(kb + 3, std::integral_constant<int, 3>(), we4, xe4);
+    aim();
+    Fp8Place cur = next;
+    fetch(0);
+    int stage = 0;
+    for (;;) {
+        f32x16_t acc[TT][4];
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int f = 0; f < 4; ++f)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[t][f][i] = 0.0f;
+        int we = 0, xe[TT] = {};
+        bool again = false;
+        Fp8Place after = cur;
+        for (int kb = 0; kb < p.nkb; ++kb, stage ^= 1) {
+            // this slab has arrived, and every wave is done with the one before
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if ((kb & 3) == 0) {
+                we = we_next;
+#pragma unroll
+                for (int t = 0; t < TT; ++t) { xe[t] = xe_next[t]; asm volatile("" : "+v"(xe[t])); }
+            }
+            if (kb + 1 == p.nkb) { after = next; again = more; }
+            if (more) fetch(stage ^ 1);
+            const uint8_t* w = smem + stage * G::STAGE + wbase;
+            const uint8_t* x = smem + stage * G::STAGE + xbase;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                i32x8_t b[TT];
+#pragma unroll
+                for (int t = 0; t < TT; ++t)
+                    b[t] = two16(*reinterpret_cast<const uint4*>(x + t * 4096 + frag[2 * s]), *reinterpret_cast<const uint4*>(x + t * 4096 + frag[2 * s + 1]));
+#pragma unroll
+                for (int f = 0; f < 4; ++f) {
+                    const i32x8_t a = two16(*reinterpret_cast<const uint4*>(w + f * 4096 + frag[2 * s]), *reinterpret_cast<const uint4*>(w + f * 4096 + frag[2 * s + 1]));
+#pragma unroll
+                    for (int t = 0; t < TT; ++t) acc[t][f] = mma<0>(a, b[t], acc[t][f], we, xe[t]);
+                }
+            }
+            we = (int)((uint32_t)we >> 8);
+#pragma unroll
+            for (int t = 0; t < TT; ++t) xe[t] = (int)((uint32_t)xe[t] >> 8);
+        }
+        if (cur.col + wf < p.nnb) {
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                const int r = cur.row + (wt * TT + t) * 32 + l32;
+                store_block<OUT>(p, acc[t], cur.col + wf, r, r < cur.end, half);
+            }
+        }
+        if (!again) break;
+        cur = after;
     }
-    store_tile<OUT>(p, acc, nb, r, live, half);
+}
+
+// compute units of the current device (looked up once per device)
+static int compute_units() {
+    static int cached[64];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+    int n = __atomic_load_n(&cached[dev], __ATOMIC_RELAXED);
+    if (n == 0) {
+        int v = 0;
+        n = (hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && v > 0) ? v : 256;
+        __atomic_store_n(&cached[dev], n, __ATOMIC_RELAXED);
+    }
+    return n;
+}
+
+template <int WF, int WT, int TT, int OUT>
+static int launch_tiles(const Fp8Args& p, int per_cu, hipStream_t st) {
+    typedef Fp8Tile<WF, WT, TT> G;
+    static unsigned long long opted;
+    const auto kern = fp8_tile_kernel<WF, WT, TT, OUT>;
+    if (!lds_opt_in((const void*)kern, G::BYTES, &opted)) return MOE_ERR_LAUNCH;
+    const long long most = ((long long)p.rows / G::BT + (p.E < p.rows ? p.E : p.rows)) * ((p.nnb + WF - 1) / WF);
+    long long wgs = (long long)compute_units() * per_cu / 8 * 8;
+    if (wgs < 8) wgs = 8;
+    if (wgs > (most + 7) / 8 * 8) wgs = (most + 7) / 8 * 8;
+    kern<<<(unsigned)wgs, G::NT, G::BYTES, st>>>(p);
+    return MOE_OK;
+}
+
+// Which kernel?  Estimated from the mean rows of the experts that can have any.
+enum { FP8_LARGE = 0, FP8_SMALL = 1, FP8_THIN = 2 };
+// 256 x 256 or 128 x 128: a CU holds one workgroup of the large tile, which works off its area a fifth faster (half the
+// operands per product), or two of the small one; either way the launch takes whole rounds of tiles.  Measured, large against
+// small, us: 131072 rows, 2048 x 8192, 16 experts: first product 2419, 2700, second 1849, 2187; 10006 rows, 776 x 3080, 6
+// experts with a Zipf gate: first 80, 64 (three rounds against four halves), second 46, 52; 4096 rows, 1024 x 4096,
+// 16 experts: first 34, 36, second (64 tiles) 53, 34.
+// 32 x 32 with an eight-way split reduction: where there are so few small tiles that one tile's reduction is the launch's
+// time, 0.6 us for each of its 128 entries, against 0.084 us for each small tile's worth of thin ones.  8 rows of 8
+// experts, 1024 x 4096: second product 23.1 us with the small tile, 10.4 thin; 2048 x 2048: 13.3, 15.7; 122 rows of 32 experts,
+// 1024 x 4096: 26.2, 41.0.
+static int fp8_kernel(int rows, int experts, int nkb, int nnb, bool hidden) {
+    const long long E = experts < rows ? experts : rows, per = (rows + E - 1) / E, cus = compute_units();
+    const long long large = E * ((per + 255) / 256) * ((nnb + 1) / 2), small = E * ((per + 127) / 128) * nnb;
+    if (!hidden && per <= 32 && 7 * (long long)nkb > 15 + small) return FP8_THIN;
+    return 40 * ((large + cus - 1) / cus) < 24 * ((small + 2 * cus - 1) / (2 * cus)) ? FP8_LARGE : FP8_SMALL;
 }
 
 template <int OUT>
-static void launch_fp8(const Fp8Args& p, hipStream_t st) {
-    const long long most = (long long)p.rows / 32 + (p.E < p.rows ? p.E : p.rows);     // row tiles, at most
-    fp8_gemm_kernel<OUT><<<(unsigned)(most * p.nnb), 64, 0, st>>>(p);
+static int launch_fp8(const Fp8Args& p, hipStream_t st) {
+    constexpr bool HIDDEN = OUT == OUT_RELU8 || OUT == OUT_GELU8;
+    const int kind = fp8_kernel(p.rows, p.E, p.nkb, p.nnb, HIDDEN);
+    if constexpr (!HIDDEN) {
+        if (kind == FP8_THIN) {
+            const long long most = (long long)p.rows / 32 + (p.E < p.rows ? p.E : p.rows);     // row tiles, at most
+            fp8_thin_kernel<OUT><<<(unsigned)(most * p.nnb * 4), 64 * THIN8_WAVES, 0, st>>>(p);
+            return MOE_OK;
+        }
+    }
+    return kind == FP8_LARGE ? launch_tiles<2, 4, 2, OUT>(p, 1, st) : launch_tiles<1, 4, 1, OUT>(p, 2, st);
+}
+
+// measurement aid: the kernels of the block's two products
+extern "C" int moe_fp8_kernels(const moe_fp8_shape* shape, int32_t* first, int32_t* second) {
+    const int rc = fp8_shape_status(shape);
+    if (rc) return rc;
+    if (!first || !second) return MOE_ERR_NULL;
+    const int R = shape->T * shape->k, d = fp8_blocks(shape->d_model), f = fp8_blocks(shape->d_ff);
+    *first = fp8_kernel(R, shape->E, d, f, true);
+    *second = fp8_kernel(R, shape->E, f, d, false);
+    return MOE_OK;
 }
 
 static Fp8Args fp8_args(int rows, int E, int K, int N, const void* xq, const uint8_t* xb, const int32_t* start, const void* wq,
@@ -202,13 +520,14 @@ static Fp8Args fp8_args(int rows, int E, int K, int N, const void* xq, const uin
 }
 
 extern "C" int moe_expert_product_fp8(int32_t rows, int32_t E, int32_t K, int32_t N, const void* xq, const uint8_t* xb,
-                                      const int32_t* expert_start, const void* Wq, const uint8_t* Wb, void* y,
-                                      void* stream) {
-    const int rc = begin_call(fp8_extent_status(rows, E, K, N, MOE_BF16));
+                                      const int32_t* expert_start, const void* Wq, const uint8_t* Wb, int32_t y_dtype,
+                                      void* y, void* stream) {
+    int rc = begin_call(fp8_extent_status(rows, E, K, N, y_dtype));
     if (rc) return rc;
     if (!xq || !xb || !expert_start || !Wq || !Wb || !y) return MOE_ERR_NULL;
-    launch_fp8<OUT_BF16>(fp8_args(rows, E, K, N, xq, xb, expert_start, Wq, Wb, y, nullptr), (hipStream_t)stream);
-    return launch_status();
+    const Fp8Args p = fp8_args(rows, E, K, N, xq, xb, expert_start, Wq, Wb, y, nullptr);
+    rc = y_dtype == MOE_BF16 ? launch_fp8<OUT_BF16>(p, (hipStream_t)stream) : launch_fp8<OUT_F32>(p, (hipStream_t)stream);
+    return rc ? rc : launch_status();
 }
 
 int fp8_shape_status(const moe_fp8_shape* s) {
@@ -219,24 +538,28 @@ int fp8_shape_status(const moe_fp8_shape* s) {
 }
 
 int ffn_fp8_check(const moe_fp8_shape* s, const void* xq, const uint8_t* xb, const int32_t* expert_start, const void* W1q,
-                  const uint8_t* W1b, const void* W2q, const uint8_t* W2b, const void* hq, const uint8_t* hb, const void* yd) {
+                  const uint8_t* W1b, const void* W2q, const uint8_t* W2b, const void* hq, const uint8_t* hb, int yd_dtype,
+                  const void* yd) {
     const int rc = fp8_shape_status(s);
-    return rc ? rc : xq && xb && expert_start && W1q && W1b && W2q && W2b && hq && hb && yd ? MOE_OK : MOE_ERR_NULL;
+    if (rc) return rc;
+    if (yd_dtype != MOE_F32 && yd_dtype != MOE_BF16) return MOE_ERR_DTYPE;
+    return xq && xb && expert_start && W1q && W1b && W2q && W2b && hq && hb && yd ? MOE_OK : MOE_ERR_NULL;
 }
 
 extern "C" int moe_expert_ffn_fwd_fp8(const moe_fp8_shape* shape, const void* xq, const uint8_t* xb,
                                       const int32_t* expert_start, const void* W1q, const uint8_t* W1b, const void* W2q,
-                                      const uint8_t* W2b, void* hq, uint8_t* hb, void* yd, void* stream) {
-    const int rc = begin_call(ffn_fp8_check(shape, xq, xb, expert_start, W1q, W1b, W2q, W2b, hq, hb, yd));
+                                      const uint8_t* W2b, void* hq, uint8_t* hb, int32_t yd_dtype, void* yd,
+                                      void* stream) {
+    int rc = begin_call(ffn_fp8_check(shape, xq, xb, expert_start, W1q, W1b, W2q, W2b, hq, hb, yd_dtype, yd));
     if (rc) return rc;
     const int R = shape->T * shape->k;
     hipStream_t st = (hipStream_t)stream;
     const Fp8Args p1 = fp8_args(R, shape->E, shape->d_model, shape->d_ff, xq, xb, expert_start, W1q, W1b, hq, hb);
-    if (shape->act == MOE_GELU) launch_fp8<OUT_GELU8>(p1, st);
-    else launch_fp8<OUT_RELU8>(p1, st);
+    rc = shape->act == MOE_GELU ? launch_fp8<OUT_GELU8>(p1, st) : launch_fp8<OUT_RELU8>(p1, st);
+    if (rc) return rc;
     const Fp8Args p2 = fp8_args(R, shape->E, shape->d_ff, shape->d_model, hq, hb, expert_start, W2q, W2b, yd, nullptr);
-    launch_fp8<OUT_BF16>(p2, st);
-    return launch_status();
+    rc = yd_dtype == MOE_BF16 ? launch_fp8<OUT_BF16>(p2, st) : launch_fp8<OUT_F32>(p2, st);
+    return rc ? rc : launch_status();
 }
 
 // ---------------------------------------------------------------------------
@@ -255,13 +578,13 @@ extern "C" int moe_layer_fwd_fp8(const moe_fp8_shape* s, const moe_router* r, in
     if (!rc) rc = router_fwd_check(r, b->logits, b->expert_idx, b->gate_w);
     if (!rc) rc = sort_check(r, b->expert_idx, b->row_of, b->expert_start, b->ws, b->ws_bytes);
     if (!rc) rc = dispatch_fp8_check(s, x, b->row_of, b->xq, b->xb);
-    if (!rc) rc = ffn_fp8_check(s, b->xq, b->xb, b->expert_start, W1q, W1b, W2q, W2b, b->hq, b->hb, b->yd);
-    if (!rc) rc = combine_rows_check(s, b->yd, b->row_of, b->gate_w, b->y);
+    if (!rc) rc = ffn_fp8_check(s, b->xq, b->xb, b->expert_start, W1q, W1b, W2q, W2b, b->hq, b->hb, MOE_F32, b->yd);
+    if (!rc) rc = combine_rows_check(s, MOE_F32, b->yd, b->row_of, b->gate_w, b->y);
     if (!rc && !logits_given) rc = moe_gate_logits(&gate, x, Wg, nullptr, b->logits, stream);
     if (!rc) rc = moe_router_fwd(r, b->logits, select_bias_or_null, token_mask_or_null, b->expert_idx, b->gate_w, stream);
     if (!rc) rc = moe_sort_choices(r, b->expert_idx, b->row_of, b->expert_start, b->ws, b->ws_bytes, stream);
     if (!rc) rc = moe_dispatch_fp8(s, x, b->row_of, b->xq, b->xb, stream);
-    if (!rc) rc = moe_expert_ffn_fwd_fp8(s, b->xq, b->xb, b->expert_start, W1q, W1b, W2q, W2b, b->hq, b->hb, b->yd, stream);
-    if (!rc) rc = moe_combine_rows(s, b->yd, b->row_of, b->gate_w, b->y, stream);
+    if (!rc) rc = moe_expert_ffn_fwd_fp8(s, b->xq, b->xb, b->expert_start, W1q, W1b, W2q, W2b, b->hq, b->hb, MOE_F32, b->yd, stream);
+    if (!rc) rc = moe_combine_rows(s, MOE_F32, b->yd, b->row_of, b->gate_w, b->y, stream);
     return rc;
 }

@@ -353,5 +353,6 @@ int sort_check(const moe_router* r, const int32_t* expert_idx, const int32_t* ro
 int fp8_shape_status(const moe_fp8_shape* s);
 int dispatch_fp8_check(const moe_fp8_shape* s, const void* x, const int32_t* row_of, const void* xq, const uint8_t* xb);
 int ffn_fp8_check(const moe_fp8_shape* s, const void* xq, const uint8_t* xb, const int32_t* expert_start, const void* W1q,
-                  const uint8_t* W1b, const void* W2q, const uint8_t* W2b, const void* hq, const uint8_t* hb, const void* yd);
-int combine_rows_check(const moe_fp8_shape* s, const void* yd, const int32_t* row_of, const float* gate_w, const void* y);
+                  const uint8_t* W1b, const void* W2q, const uint8_t* W2b, const void* hq, const uint8_t* hb, int yd_dtype,
+                  const void* yd);
+int combine_rows_check(const moe_fp8_shape* s, int yd_dtype, const void* yd, const int32_t* row_of, const float* gate_w, const void* y);

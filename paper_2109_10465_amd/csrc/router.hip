@@ -443,10 +443,18 @@ extern "C" int moe_router_bias_update(const moe_router* router, const int32_t* e
 // ---------------------------------------------------------------------------
 // mixture of a token's rows: one wave per token, 16-byte vectors
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void combine_rows_kernel(int Tn, int d, int k, int R, const bf16_t* __restrict__ yd,
+// 8 entries of a row of yd
+__device__ __forceinline__ void row8(const bf16_t* p, float (&v)[8]) { Chunk<bf16_t>::load(p, v); }
+__device__ __forceinline__ void row8(const float* p, float (&v)[8]) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void combine_rows_kernel(int Tn, int d, int k, int R, const T* __restrict__ yd,
                                                            const int32_t* __restrict__ row_of,
                                                            const float* __restrict__ gate_w, bf16_t* __restrict__ y) {
-    constexpr int CN = Chunk<bf16_t>::N;
     const int lane = threadIdx.x & 63, t = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (t >= Tn) return;
     int row[ROUTER_MAX_K];
@@ -457,33 +465,39 @@ __global__ __launch_bounds__(256) void combine_rows_kernel(int Tn, int d, int k,
         row[j] = (unsigned)r < (unsigned)R ? r : -1;
         w[j] = row[j] >= 0 ? gate_w[(size_t)t * k + j] : 0.0f;
     }
-    const int nvec = d / CN;
-    for (int v = lane; v < nvec; v += 64) {
-        float acc[CN];
+    for (int v = lane; v < d / 8; v += 64) {
+        float acc[8];
 #pragma unroll
-        for (int i = 0; i < CN; ++i) acc[i] = 0.0f;
+        for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
 #pragma unroll
         for (int j = 0; j < ROUTER_MAX_K; ++j) {
             if (row[j] < 0) continue;
-            float b[CN];
-            Chunk<bf16_t>::load(yd + (size_t)row[j] * d + (size_t)v * CN, b);
+            float b[8];
+            row8(yd + (size_t)row[j] * d + (size_t)v * 8, b);
 #pragma unroll
-            for (int i = 0; i < CN; ++i) acc[i] = fmaf(w[j], b[i], acc[i]);
+            for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], b[i], acc[i]);
         }
-        Chunk<bf16_t>::store(y + (size_t)t * d + (size_t)v * CN, acc);
+        Chunk<bf16_t>::store(y + (size_t)t * d + (size_t)v * 8, acc);
     }
 }
 
-int combine_rows_check(const moe_fp8_shape* s, const void* yd, const int32_t* row_of, const float* gate_w, const void* y) {
+int combine_rows_check(const moe_fp8_shape* s, int yd_dtype, const void* yd, const int32_t* row_of, const float* gate_w,
+                       const void* y) {
     const int rc = fp8_shape_status(s);
-    return rc ? rc : yd && row_of && gate_w && y ? MOE_OK : MOE_ERR_NULL;
+    if (rc) return rc;
+    if (yd_dtype != MOE_F32 && yd_dtype != MOE_BF16) return MOE_ERR_DTYPE;
+    return yd && row_of && gate_w && y ? MOE_OK : MOE_ERR_NULL;
 }
 
-extern "C" int moe_combine_rows(const moe_fp8_shape* shape, const void* yd, const int32_t* row_of,
+extern "C" int moe_combine_rows(const moe_fp8_shape* shape, int32_t yd_dtype, const void* yd, const int32_t* row_of,
                                 const float* gate_w, void* y, void* stream) {
-    const int rc = begin_call(combine_rows_check(shape, yd, row_of, gate_w, y));
+    const int rc = begin_call(combine_rows_check(shape, yd_dtype, yd, row_of, gate_w, y));
     if (rc) return rc;
-    combine_rows_kernel<<<ceil_div(shape->T, 4), 256, 0, (hipStream_t)stream>>>(
-        shape->T, shape->d_model, shape->k, shape->T * shape->k, (const bf16_t*)yd, row_of, gate_w, (bf16_t*)y);
+    const int grid = ceil_div(shape->T, 4), R = shape->T * shape->k;
+    hipStream_t st = (hipStream_t)stream;
+    if (yd_dtype == MOE_BF16)
+        combine_rows_kernel<bf16_t><<<grid, 256, 0, st>>>(shape->T, shape->d_model, shape->k, R, (const bf16_t*)yd, row_of, gate_w, (bf16_t*)y);
+    else
+        combine_rows_kernel<float><<<grid, 256, 0, st>>>(shape->T, shape->d_model, shape->k, R, (const float*)yd, row_of, gate_w, (bf16_t*)y);
     return launch_status();
 }

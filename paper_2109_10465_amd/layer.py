@@ -164,7 +164,7 @@ class Fp8MoELayer:
                 raise B.MoeError("8-bit weights must be contiguous")
         self.W1, self.W2 = W1, W2
         self.device = torch.device(device)
-        adt, R = _TORCH_DT[dtype], T * k
+        R = T * k
 
         def buf(shape, dt):
             return torch.empty(shape, dtype=dt, device=self.device)
@@ -175,7 +175,7 @@ class Fp8MoELayer:
         self.expert_start = buf((E + 1,), torch.int32)
         self.xq, self.xb = buf((R, B.fp8_padded(d_model)), u8), buf((R, B.fp8_scale_bytes(d_model)), u8)
         self.hq, self.hb = buf((R, B.fp8_padded(d_ff)), u8), buf((R, B.fp8_scale_bytes(d_ff)), u8)
-        self.yd, self.y = buf((R, d_model), adt), buf((T, d_model), adt)
+        self.yd, self.y = buf((R, d_model), torch.float32), buf((T, d_model), _TORCH_DT[dtype])
         self.ws = buf((nbytes,), u8)
 
     @staticmethod

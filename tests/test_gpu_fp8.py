@@ -110,8 +110,9 @@ def exact_product(xq, xb, wq, wb, counts, N):
 
 
 def close(got, want, off):
-    """... and bfloat16's rounding on top."""
-    assert ((got.cpu().double() - want).abs() <= off + 2.0 ** -8 * (want.abs() + off)).all()
+    """... and the result's own rounding on top."""
+    u = 2.0 ** -8 if got.dtype == torch.bfloat16 else 2.0 ** -24
+    assert ((got.cpu().double() - want).abs() <= off + u * (want.abs() + off)).all()
 
 
 COUNTS = [(1,), (3, 0, 2), (0, 0, 40, 1), (33, 31, 32, 64, 65), (257, 5, 0, 100), (300,), (129,) * 3, (1,) * 70, (0,) * 9 + (7,)]
@@ -119,11 +120,12 @@ COUNTS = [(1,), (3, 0, 2), (0, 0, 40, 1), (33, 31, 32, 64, 65), (257, 5, 0, 100)
 
 @pytest.mark.parametrize("counts", COUNTS, ids=lambda c: f"{len(c)}e{sum(c)}")
 @pytest.mark.parametrize("K,N", [(8, 8), (128, 128), (136, 264), (512, 72), (1160, 520), (2048, 256)])
-def test_product(counts, K, N):
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_product(counts, K, N, dtype):
     rows = sum(counts) + 3
     xq, xb, wq, wb = operands(counts, K, N, K + N, rows)
-    y = torch.full((rows, N), -7.0, dtype=torch.bfloat16, device="cuda")
-    print(f"[gpu] product {counts[:6]} K={K} N={N}", flush=True)
+    y = torch.full((rows, N), -7.0, dtype=dtype, device="cuda")
+    print(f"[gpu] product {counts[:6]} K={K} N={N} {dtype}", flush=True)
     B.moe_expert_product_fp8(rows, len(counts), K, N, xq, xb, starts(counts), wq, wb, y)
     torch.cuda.synchronize()
     want, off = exact_product(xq, xb, wq, wb, counts, N)
@@ -133,7 +135,8 @@ def test_product(counts, K, N):
 
 
 @pytest.mark.parametrize("counts,K,N", [((700, 900, 300), 640, 776), ((4000,), 384, 256), ((40,) * 100, 256, 384), ((8,) * 256, 520, 128),
-                                        ((2500, 100, 0, 1), 1024, 1032)])
+                                        ((2500, 100, 0, 1), 1024, 1032), ((4000,), 384, 4096), ((2500, 1200, 0, 700), 1160, 2056),
+                                        ((257,) * 64, 136, 1048)])
 def test_larger_products(counts, K, N):
     xq, xb, wq, wb = operands(counts, K, N, K + N)
     y = torch.empty((sum(counts), N), dtype=torch.bfloat16, device="cuda")
@@ -142,6 +145,14 @@ def test_larger_products(counts, K, N):
     torch.cuda.synchronize()
     want, off = exact_product(xq, xb, wq, wb, counts, N)
     close(y, want, off)
+
+
+def test_every_kernel_is_reached_above():
+    kinds = lambda counts, d, f: B.moe_fp8_kernels(B.make_fp8_shape(sum(counts), d, f, len(counts), 1, B.BF16, B.GELU))
+    assert kinds((2500, 1200, 0, 700), 264, 2056)[0] == 0 and kinds((900, 700, 800), 256, 512) == (1, 1)
+    # as products: K is the reduction, which is d_ff for the second
+    assert kinds((4000,), 4096, 384)[1] == kinds((2500, 1200, 0, 700), 2056, 1160)[1] == 0
+    assert kinds((1,), 264, 2048)[1] == kinds((3, 0, 2, 3), 264, 1160)[1] == 2
 
 
 def test_exponents_at_their_ends():
@@ -181,23 +192,25 @@ def test_starts_outside_of_the_rows_are_clamped():
 
 @pytest.mark.parametrize("act", [B.RELU, B.GELU])
 @pytest.mark.parametrize("counts,d,f", [((1,), 8, 8), ((5, 0, 40), 136, 264), ((64, 70, 3, 1), 256, 1032), ((300, 20), 392, 640),
-                                        ((20,) * 60, 128, 520), ((900, 700, 800), 256, 512)])
-def test_block(act, counts, d, f):
+                                        ((20,) * 60, 128, 520), ((900, 700, 800), 256, 512), ((2500, 1200, 0, 700), 264, 2056)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_block(act, counts, d, f, dtype):
     T, E = sum(counts), len(counts)
     xq, xb, w1q, w1b = operands(counts, d, f, d + f, wstd=0.5 / d ** 0.5)
     _, _, w2q, w2b = operands(counts, f, d, f, rows=1)
     s = B.make_fp8_shape(T, d, f, E, 1, B.BF16, act)
     hq = torch.full((T, B.fp8_padded(f)), 0x55, dtype=U8, device="cuda")
     hb = torch.full((T, B.fp8_scale_bytes(f)), 0x55, dtype=U8, device="cuda")
-    yd = torch.empty((T, d), dtype=torch.bfloat16, device="cuda")
+    yd = torch.empty((T, d), dtype=dtype, device="cuda")
     print(f"[gpu] block {counts[:6]} d={d} f={f} act={act}", flush=True)
     B.moe_expert_ffn_fwd_fp8(s, xq, xb, starts(counts), w1q, w1b, w2q, w2b, hq, hb, yd)
     torch.cuda.synchronize()
     z, zoff = exact_product(xq, xb, w1q, w1b, counts, f)
     h = torch.zeros(T, B.fp8_padded(f), dtype=torch.float64)
     h[:, :f] = R.act(z, act == B.GELU)
-    off = torch.zeros_like(h)       # of h in fp32: the sum's (|act'| < 1.13) and the activation's own
-    off[:, :f] = 1.13 * zoff + 2.0 ** -21 * h[:, :f].abs() + 1e-7 * z.abs()
+    # of h in fp32: the sum's (|act'| < 1.13) and the activation's own (gelu's fit is 1.1e-6 off at most, computed in fp32)
+    off = torch.zeros_like(h)
+    off[:, :f] = 1.13 * zoff + 2.0 ** -21 * h[:, :f].abs() + 1.2e-6 * (act == B.GELU)
     nb = f // 128 + (f % 128 > 0)
     top, slack = h.abs().reshape(T, nb, 128).amax(2), off.reshape(T, nb, 128).amax(2)
     lo, hi = R.exponent((top - slack).clamp(min=0)), R.exponent(top + slack)
@@ -229,7 +242,8 @@ def test_block_with_infinite_and_nan_rows():
 
 
 @pytest.mark.parametrize("T,k,d", [(1, 1, 8), (5, 8, 136), (70, 3, 520), (333, 2, 1024)])
-def test_dispatch_and_combine(T, k, d):
+@pytest.mark.parametrize("yd_dtype", [torch.bfloat16, torch.float32])
+def test_dispatch_and_combine(T, k, d, yd_dtype):
     dtype = torch.bfloat16
     rng = np.random.default_rng(T)
     x = values((T, d), T + d, dtype)
@@ -242,7 +256,7 @@ def test_dispatch_and_combine(T, k, d):
     rows = torch.from_numpy(row).cuda()
     print(f"[gpu] dispatch T={T} k={k} d={d}", flush=True)
     B.moe_dispatch_fp8(s, x.cuda(), rows, q, b)
-    yd = values((T * k, d), 3, dtype)
+    yd = values((T * k, d), 3, yd_dtype)
     ok = (row >= 0) & (row < T * k)
     unused = np.setdiff1d(np.arange(T * k), row[ok])
     yd[unused] = float("nan")
@@ -306,12 +320,12 @@ def test_whole_pass(T, d, f, E, k, groups, top, act):
                     h, o = R.act(z, act == B.GELU), m2[e][:f, :d]
                     want += float(w[t, j]) * (h @ o)
                     zoff = 7 * 2.0 ** -13 * (xw[t].abs().reshape(-1, 8).amax(1) @ m1[e][:d, :f].abs().reshape(d // 8, 8, f).amax(1))
-                    hoff = 1.13 * zoff + 2.0 ** -20 * z.abs()
+                    hoff = 1.13 * zoff + 2.0 ** -20 * z.abs() + 1.2e-6
                     # a block's unit is at most 2 / 448 of its largest value; the whole row's largest bounds it
                     hoff = hoff + torch.maximum(2.0 ** -4 * (h.abs() + hoff), 2.0 ** -9 / 448 * (h.abs() + hoff).max())
                     ho = (h.abs() + hoff).reshape(-1, 8).amax(1) @ o.abs().reshape(f // 8, 8, d).amax(1)
-                    mag += float(w[t, j]) * (hoff @ o.abs() + 8 * 2.0 ** -13 * ho + 2.0 ** -8 * (h @ o).abs())
-            tol = mag + 2.0 ** -8 * (want.abs() + 2 * mag)      # rows and their sum are bfloat16
+                    mag += float(w[t, j]) * (hoff @ o.abs() + 8 * 2.0 ** -13 * ho)
+            tol = mag + 2.0 ** -8 * (want.abs() + mag)
             assert ((y[t].cpu().double() - want).abs() <= tol).all(), t
             if not mask[t]:
                 assert not y[t].any()

@@ -73,18 +73,22 @@ BAD_SHAPE = [(dict(T=0), -2), (dict(k=0), -2), (dict(k=9), -2), (dict(E=0), -2),
 def test_fp8_shape(over, code):
     L, s = B.lib(), shape(**over)
     assert L.moe_dispatch_fp8(REF(s), P, P, P, P, None) == code
-    assert L.moe_expert_ffn_fwd_fp8(REF(s), *[P] * 10, None) == code
-    assert L.moe_combine_rows(REF(s), *[P] * 4, None) == code
+    assert L.moe_expert_ffn_fwd_fp8(REF(s), *[P] * 9, 1, P, None) == code
+    assert L.moe_combine_rows(REF(s), 1, *[P] * 4, None) == code
 
 
 def test_fp8_pointers():
     L, s = B.lib(), shape()
-    for f, n in ((L.moe_dispatch_fp8, 4), (L.moe_expert_ffn_fwd_fp8, 10), (L.moe_combine_rows, 4)):
+    ffn = lambda s, *a: L.moe_expert_ffn_fwd_fp8(s, *a[:9], 0, *a[9:])
+    combine = lambda s, *a: L.moe_combine_rows(s, 0, *a)
+    for f, n in ((L.moe_dispatch_fp8, 4), (ffn, 10), (combine, 4)):
         assert f(None, *[P] * n, None) == -1
         for i in range(n):
             a = [P] * n
             a[i] = None
             assert f(REF(s), *a, None) == -1
+    assert L.moe_expert_ffn_fwd_fp8(REF(s), *[P] * 9, 2, P, None) == -3
+    assert L.moe_combine_rows(REF(s), 2, *[P] * 4, None) == -3
     for i in range(3):
         a = [P] * 3
         a[i] = None
@@ -93,7 +97,7 @@ def test_fp8_pointers():
     for i in range(6):
         a = [P] * 6
         a[i] = None
-        assert L.moe_expert_product_fp8(4, 2, 128, 64, *a, None) == -1
+        assert L.moe_expert_product_fp8(4, 2, 128, 64, *a[:5], 1, a[5], None) == -1
 
 
 @pytest.mark.parametrize("rows,E,K,N,dtype,code", [(0, 1, 128, 128, 0, -2), (1 << 30, 1, 128, 128, 0, -2), (4, 1, 12, 128, 0, -2),
@@ -101,8 +105,7 @@ def test_fp8_pointers():
                                                    (4, 1, 1 << 20, 1 << 12, 1, -2)])
 def test_fp8_extents(rows, E, K, N, dtype, code):
     L = B.lib()
-    if dtype != 2:
-        assert L.moe_expert_product_fp8(rows, E, K, N, *[P] * 6, None) == code
+    assert L.moe_expert_product_fp8(rows, E, K, N, *[P] * 5, dtype, P, None) == code
     if rows == 4:
         assert L.moe_quantise_weights_fp8(E, K, N, dtype, P, P, P, None) == code
     if N == 128 and E == 1:
@@ -169,7 +172,3 @@ def test_extents_of_the_8_bit_format():
     assert [B.fp8_padded(n) for n in (8, 128, 136)] == [128, 128, 256]
     assert [B.fp8_scale_bytes(n) for n in (8, 512, 520, 2048)] == [4, 4, 8, 16]
 
-
-def test_products_are_bfloat16_only():
-    with pytest.raises(B.MoeError):
-        B.moe_expert_product_fp8(1, 1, 8, 8, None, None, None, None, None, torch.zeros(1, 8))

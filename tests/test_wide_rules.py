@@ -1,0 +1,26 @@
+"""Which kernels the rules of the 8-bit products choose, at shapes where both sides have been measured (host-only queries; the
+times are microseconds on an MI355X)."""
+import pytest
+
+from paper_2109_10465_amd import binding as B
+
+
+@pytest.mark.parametrize("T,k,d,f,E,kinds", [
+    (65536, 2, 2048, 8192, 16, (0, 0)),     # large 2419, 1849; small 2700, 2187
+    (5003, 2, 776, 3080, 6, (1, 0)),        # large 80, 46; small 64, 52
+    (7375, 4, 1024, 4096, 64, (0, 0)),      # large 192, 145; small 227, 171
+    (2048, 2, 1024, 4096, 16, (0, 1)),      # large 34, 53; small 36, 34
+    (2048, 2, 1024, 4096, 32, (1, 1)),      # large 67, 52; small 48, 45
+    (61, 2, 1024, 4096, 32, (1, 1)),        # second: small 26, thin 41
+    (1, 8, 1024, 4096, 8, (1, 2)),          # 23, 10
+    (1, 8, 2048, 2048, 8, (1, 1)),          # 13, 16
+    (16, 1, 1024, 2048, 128, (1, 1)),       # 13, 16
+])
+def test_kernels_of_the_block(T, k, d, f, E, kinds):
+    for act in (B.RELU, B.GELU):
+        assert B.moe_fp8_kernels(B.make_fp8_shape(T, d, f, E, k, B.BF16, act)) == kinds
+
+
+def test_query_refuses_what_the_block_refuses():
+    with pytest.raises(B.MoeError):
+        B.moe_fp8_kernels(B.make_fp8_shape(1, 12, 16, 1, 1, B.BF16, B.GELU))
