@@ -10,12 +10,21 @@
 // ---------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------
-// LPT lanes share a token and hold Q consecutive experts of one group each: group g has the Lg lanes from
-// g * Lg on, so the order of (lane, entry) is the order of the ids, whatever the groups' size.
+// LPT lanes share a token and hold eight consecutive experts of one group each: group g has the 2^lg_log2 lanes from
+// there on, so the order of (lane, entry) is the order of the ids, whatever the groups' size.
+//
+// The choice is one of values in 64 bits.  It is made on keys of 32 bits, whose last three bits name the lane's entry:
+// a lane sorts its eight keys, and a round takes the largest head of the token's lanes, whose owner notes the expert
+// and moves on to its next key.  Where two values that matter - a choice and the next one, two groups - lie nearer
+// together than keys and fp32 scores can be off, the wave makes its choices again in 64 bits (about 1 in 100
+// tokens of 256 experts; equal logits always).  What bounds it is the number of vector instructions, 660 for the two
+// tokens of a wave at 65536 tokens of 256 experts in 8 groups, top 8: 55 us, where all values in 64 bits took 190 and
+// the logits' read takes 12.
 struct RouterArgs {
     int T, E, k, score, n_groups, group, top_groups, group_best, renormalise;   // group = experts per group
     float scale;
-    int lg_log2, lpt_log2;          // lanes per group and per token
+    int lg_log2;                    // lanes per group
+    int vec;                        // a lane's experts start on 16 bytes and are eight
 };
 
 __device__ __forceinline__ double score64(double l, bool sigmoid, double top, double total) {
@@ -26,210 +35,310 @@ template <typename V> __device__ __forceinline__ bool ahead(V va, int ia, V vb, 
     return va > vb || (va == vb && ia < ib);
 }
 
-// V: what the choice compares - the logits themselves (float), or score + bias (double)
-template <int Q, typename V>
-__global__ __launch_bounds__(256) void router_fwd_kernel(const RouterArgs a, const float* __restrict__ logits,
-                                                         const float* __restrict__ bias, const uint8_t* __restrict__ mask,
-                                                         int32_t* __restrict__ expert_idx, float* __restrict__ gate_w) {
-    constexpr bool BIAS = sizeof(V) == 8;
-    const int lpt = 1 << a.lpt_log2, lg = 1 << a.lg_log2;
-    const int sub = threadIdx.x & (lpt - 1), t = blockIdx.x * (256 >> a.lpt_log2) + (threadIdx.x >> a.lpt_log2);
-    const int g = sub >> a.lg_log2, first = (sub & (lg - 1)) * Q, e0 = g * a.group + first;
-    const int here = g < a.n_groups ? min(max(a.group - first, 0), Q) : 0;
-    const bool in = t < a.T, valid = in && (!mask || mask[t] != 0);
-    const bool sigmoid = a.score == MOE_SIGMOID;
-    const float* row = logits + (size_t)(in ? t : 0) * a.E;
-    float l[Q];
-#pragma unroll
-    for (int i = 0; i < Q; ++i) {
-        l[i] = valid && i < here ? row[e0 + i] : -INFINITY;
-        if (!(l[i] == l[i])) l[i] = -INFINITY;
+#define KEY_DEAD -3.0e38f       // an expert whose logit is -inf or NaN: after every other one (also without a finite value)
+#define KEY_OUT -3.3e38f        // one that cannot be chosen
+
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+// the largest value (sum) of the LPT lanes of a token, in all of them
+template <int LPT, typename F> __device__ __forceinline__ float token_reduce(float v, F f) {
+    v = f(v, dpp<0xB1>(v));                         // lanes 1 apart, 2 apart
+    v = f(v, dpp<0x4E>(v));
+    v = f(v, dpp<0x141>(v));                        // halves of eight mirrored, then of sixteen
+    if constexpr (LPT >= 16) v = f(v, dpp<0x140>(v));
+    if constexpr (LPT >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
     }
-    // the softmax's largest logit and sum, where scores are compared or not divided by the chosen ones' sum
-    float top = 0.0f;
-    double total = 1.0;
-    if (!sigmoid) {
-        top = l[0];
+    if constexpr (LPT >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    return v;
+}
+template <int LPT> __device__ __forceinline__ float token_max(float v) { return token_reduce<LPT>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int LPT> __device__ __forceinline__ float token_sum(float v) { return token_reduce<LPT>(v, [](float a, float b) { return a + b; }); }
+
+// The choices of the wave's tokens in 64 bits, into s_choice.  (The logits are read again: nothing is kept for this.)
+template <int LPT, bool BIAS>
+__device__ __forceinline__ void choose64(const RouterArgs& a, const float* __restrict__ row, const float* __restrict__ bias,
+                                         bool valid, int here, int e0, int g, int sub, int32_t* s_choice) {
+    float l[8];
 #pragma unroll
-        for (int i = 1; i < Q; ++i) top = fmaxf(top, l[i]);
-        for (int o = lpt >> 1; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, MOE_WAVE));
-        if (top == -INFINITY) top = 0.0f;
+    for (int i = 0; i < 8; ++i) {
+        l[i] = valid && i < here ? row[e0 + i] : -INFINITY;
+        l[i] = l[i] == l[i] ? l[i] : -INFINITY;
+    }
+    const bool sigmoid = a.score == MOE_SIGMOID;
+    const int lg = 1 << a.lg_log2;
+    double top = 0.0, total = 1.0;
+    if (!sigmoid) {
+        float m = l[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) m = fmaxf(m, l[i]);
+        m = token_max<LPT>(m);
+        top = m == -INFINITY ? 0.0 : (double)m;
         total = 0.0;
 #pragma unroll
-        for (int i = 0; i < Q; ++i) total += exp((double)l[i] - (double)top);
-        for (int o = lpt >> 1; o > 0; o >>= 1) total += __shfl_xor(total, o, MOE_WAVE);
+        for (int i = 0; i < 8; ++i) total += exp((double)l[i] - top);
+        for (int o = LPT >> 1; o > 0; o >>= 1) total += __shfl_xor(total, o, MOE_WAVE);
         if (!(total > 0.0)) total = 1.0;
     }
-    V v[Q];
-    unsigned left = (1u << here) - 1u;          // experts that can still be chosen
+    double v[8];
 #pragma unroll
-    for (int i = 0; i < Q; ++i) {
+    for (int i = 0; i < 8; ++i) {
+        v[i] = l[i];
         if constexpr (BIAS) {
-            v[i] = -INFINITY;
-            if (valid && i < here && l[i] > -INFINITY) {
-                const double w = score64(l[i], sigmoid, top, total) + (double)bias[e0 + i];
-                if (w == w) v[i] = w;
-            }
-        } else {
-            v[i] = l[i];
+            const double w = score64(l[i], sigmoid, top, total) + (i < here ? (double)bias[e0 + i] : 0.0);
+            v[i] = l[i] > -INFINITY && w == w ? w : -INFINITY;
         }
     }
+    unsigned left = (1u << here) - 1u;          // experts that can still be chosen
     if (a.n_groups > 1) {
-        V b0 = -INFINITY, b1 = -INFINITY;
+        double b0 = -INFINITY, b1 = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < Q; ++i) {
+        for (int i = 0; i < 8; ++i) {
             if (v[i] > b0) { b1 = b0; b0 = v[i]; } else if (v[i] > b1) b1 = v[i];
         }
         for (int o = lg >> 1; o > 0; o >>= 1) {
-            const V c0 = __shfl_xor(b0, o, MOE_WAVE), c1 = __shfl_xor(b1, o, MOE_WAVE);
-            const V lo = b0 < c0 ? b0 : c0;
+            const double c0 = __shfl_xor(b0, o, MOE_WAVE), c1 = __shfl_xor(b1, o, MOE_WAVE);
+            const double lo = b0 < c0 ? b0 : c0;
             b0 = b0 < c0 ? c0 : b0;
             b1 = b1 < c1 ? c1 : b1;
             b1 = b1 < lo ? lo : b1;
         }
-        double gv = (double)b0;
+        double gv = b0;
         if (a.group_best == 2) {
             if constexpr (BIAS) gv = b0 + b1;
-            else gv = b1 == -INFINITY ? -INFINITY
-                                      : score64(b0, sigmoid, top, total) + score64(b1, sigmoid, top, total);
+            else gv = b1 == -INFINITY ? -INFINITY : score64(b0, sigmoid, top, total) + score64(b1, sigmoid, top, total);
         }
         if (!(gv == gv) || g >= a.n_groups) gv = -INFINITY;
         int before = 0;                         // groups in front of this one
-        for (int o = 1; o < lpt >> a.lg_log2; ++o) {
+        for (int o = 1; o < LPT >> a.lg_log2; ++o) {
             const double w = __shfl_xor(gv, o << a.lg_log2, MOE_WAVE);
             before += (g ^ o) < a.n_groups && ahead(w, g ^ o, gv, g);
         }
         if (before >= a.top_groups) left = 0;
     }
-    int choice[ROUTER_MAX_K];
-#pragma unroll
-    for (int j = 0; j < ROUTER_MAX_K; ++j) {
-        choice[j] = 0;
-        if (j >= a.k) continue;
-        V best = -INFINITY;
+    for (int j = 0; j < a.k; ++j) {
+        double best = -INFINITY;
         int id = 0x7fffffff;
 #pragma unroll
-        for (int i = 0; i < Q; ++i)
+        for (int i = 0; i < 8; ++i)
             if ((left >> i & 1u) && ahead(v[i], e0 + i, best, id)) { best = v[i]; id = e0 + i; }
-        for (int o = lpt >> 1; o > 0; o >>= 1) {
-            const V w = __shfl_xor(best, o, MOE_WAVE);
+        for (int o = LPT >> 1; o > 0; o >>= 1) {
+            const double w = __shfl_xor(best, o, MOE_WAVE);
             const int wi = __shfl_xor(id, o, MOE_WAVE);
             if (ahead(w, wi, best, id)) { best = w; id = wi; }
         }
-        choice[j] = id;
+        if (sub == 0) s_choice[j] = id;
         if (id >= e0 && id < e0 + here) left &= ~(1u << (id - e0));
     }
-    if (!in || sub != 0) return;
-    if (!valid) {
-        for (int j = 0; j < a.k; ++j) {
-            expert_idx[(size_t)t * a.k + j] = -1;
-            gate_w[(size_t)t * a.k + j] = 0.0f;
+}
+
+template <int LPT, bool BIAS>
+__global__ __launch_bounds__(256) void router_fwd_kernel(const RouterArgs a, const float* __restrict__ logits,
+                                                         const float* __restrict__ bias, const uint8_t* __restrict__ mask,
+                                                         int32_t* __restrict__ expert_idx, float* __restrict__ gate_w) {
+    static_assert(LPT >= ROUTER_MAX_K, "a lane for every choice");
+    __shared__ int32_t s_all[256 / LPT][ROUTER_MAX_K];
+    const int lg = 1 << a.lg_log2;
+    const int sub = threadIdx.x & (LPT - 1), t = blockIdx.x * (256 / LPT) + threadIdx.x / LPT;
+    const int g = sub >> a.lg_log2, first = (sub & (lg - 1)) * 8, e0 = g * a.group + first;
+    const int here = g < a.n_groups ? min(max(a.group - first, 0), 8) : 0;
+    const bool in = t < a.T, valid = in && (!mask || mask[t] != 0);
+    const bool sigmoid = a.score == MOE_SIGMOID;
+    const float* row = logits + (size_t)(in ? t : 0) * a.E;
+    int32_t* s_choice = s_all[threadIdx.x / LPT];
+    float l[8], b[8];
+    if (a.vec) {
+        float4 p = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY), q = p;
+        if (valid && here) {
+            p = *reinterpret_cast<const float4*>(row + e0);
+            q = *reinterpret_cast<const float4*>(row + e0 + 4);
         }
-        return;
-    }
-    float cl[ROUTER_MAX_K], most = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < ROUTER_MAX_K; ++j) {
-        cl[j] = j < a.k ? row[choice[j]] : -INFINITY;
-        most = fmaxf(most, cl[j]);
-    }
-    // renormalised scores, scaled so that the largest is near 1: exp(l - most), or 1 / (e^-M + e^(-l - M)) with M = max(0, -most)
-    float s[ROUTER_MAX_K], sum = 0.0f;
-    const float m = a.renormalise ? fmaxf(0.0f, -most) : 0.0f, em = expf(-m);
-#pragma unroll
-    for (int j = 0; j < ROUTER_MAX_K; ++j) {
-        if (cl[j] == -INFINITY || (sigmoid && cl[j] < LOGISTIC_ZERO)) s[j] = 0.0f;
-        else if (sigmoid) s[j] = 1.0f / (em + expf(-cl[j] - m));
-        else s[j] = a.renormalise ? expf(cl[j] - most) : (float)(exp((double)cl[j] - (double)top) / total);
-        sum += s[j];
-    }
-    const float c = !a.renormalise ? a.scale : sum == 0.0f ? 0.0f : a.scale / sum;
-#pragma unroll
-    for (int j = 0; j < ROUTER_MAX_K; ++j) {
-        if (j < a.k) {
-            expert_idx[(size_t)t * a.k + j] = choice[j];
-            gate_w[(size_t)t * a.k + j] = s[j] * c;
+        l[0] = p.x; l[1] = p.y; l[2] = p.z; l[3] = p.w; l[4] = q.x; l[5] = q.y; l[6] = q.z; l[7] = q.w;
+        p = q = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (BIAS && here) {
+            p = *reinterpret_cast<const float4*>(bias + e0);
+            q = *reinterpret_cast<const float4*>(bias + e0 + 4);
         }
+        b[0] = p.x; b[1] = p.y; b[2] = p.z; b[3] = p.w; b[4] = q.x; b[5] = q.y; b[6] = q.z; b[7] = q.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            l[i] = valid && i < here ? row[e0 + i] : -INFINITY;
+            b[i] = BIAS && i < here ? bias[e0 + i] : 0.0f;
+        }
+    }
+    // the softmax's largest logit and sum, where scores are compared or not divided by the chosen ones' sum
+    const bool sums = a.n_groups > 1 && a.group_best == 2;
+    float top = 0.0f, total = 1.0f;
+    if (!sigmoid && (BIAS || sums || !a.renormalise)) {
+        top = l[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) top = fmaxf(top, l[i]);
+        top = token_max<LPT>(top);
+        if (top == -INFINITY) top = 0.0f;
+        total = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) total += __expf(l[i] - top);
+        total = token_sum<LPT>(total);
+        if (!(total > 0.0f)) total = 1.0f;
+    }
+    const float inv = 1.0f / total;
+    auto score = [&](float x) { return sigmoid ? __builtin_amdgcn_rcpf(1.0f + __expf(-x)) : __expf(x - top) * inv; };
+    // The keys, sorted (Batcher's network of 19 comparisons).  An entry without an expert has a dead one's key: where such a
+    // key is chosen there are others like it, and the choice is made again in 64 bits.
+    float key[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float v = BIAS ? score(l[i]) + b[i] : l[i];
+        v = __builtin_amdgcn_fmed3f(v, -2.9e38f, 2.9e38f);
+        v = l[i] > -INFINITY ? v : KEY_DEAD;        // (also NaN)
+        key[i] = __uint_as_float((__float_as_uint(v) & ~7u) | (uint32_t)i);
+    }
+    auto order = [&](int i, int j) {
+        const float hi = fmaxf(key[i], key[j]), lo = fminf(key[i], key[j]);
+        key[i] = hi;
+        key[j] = lo;
+    };
+    order(0, 1); order(2, 3); order(4, 5); order(6, 7);
+    order(0, 2); order(1, 3); order(4, 6); order(5, 7);
+    order(1, 2); order(5, 6); order(0, 4); order(3, 7);
+    order(1, 5); order(2, 6);
+    order(1, 4); order(3, 6);
+    order(2, 4); order(3, 5);
+    order(3, 4);
+    // How far apart two values have to be: a key drops three bits (2^-20 of its size), a score is off by less than 5e-7
+    // (exponential, reciprocal and their argument), the sum with the bias by 2^-24: twice that, and a half more.
+    auto near = [](float hi, float lo) { return hi - lo <= fmaf(fabsf(hi) + fabsf(lo), 1.6e-6f, 1.6e-6f); };
+    bool again = false;
+    if (a.n_groups > 1) {
+        float b0 = key[0], b1 = key[1];
+        for (int o = lg >> 1; o > 0; o >>= 1) {
+            const float c0 = __shfl_xor(b0, o, MOE_WAVE), c1 = __shfl_xor(b1, o, MOE_WAVE);
+            b1 = fmaxf(fmaxf(b1, c1), fminf(b0, c0));
+            b0 = fmaxf(b0, c0);
+        }
+        float gv = b0;
+        if (a.group_best == 2) gv = b1 < -2.95e38f ? KEY_DEAD : BIAS ? b0 + b1 : score(b0) + score(b1);
+        if (g >= a.n_groups) gv = KEY_OUT;
+        int before = 0;
+        for (int o = 1; o < LPT >> a.lg_log2; ++o) {
+            const float w = __shfl_xor(gv, o << a.lg_log2, MOE_WAVE);
+            before += w > gv;
+            again |= (g ^ o) < a.n_groups && g < a.n_groups && near(fmaxf(w, gv), fminf(w, gv));
+        }
+        if (before >= a.top_groups) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) key[i] = KEY_OUT;
+        }
+    }
+    float mine = 0.0f, behind = 0.0f;       // lane j: the j-th choice and the one after it
+    for (int j = 0; j <= a.k; ++j) {        // one more than are chosen
+        const float w = token_max<LPT>(key[0]);
+        mine = sub == j ? w : mine;
+        behind = sub + 1 == j ? w : behind;
+        if (j == a.k) break;
+        if (key[0] == w) {
+            s_choice[j] = e0 + (int)(__float_as_uint(w) & 7u);
+#pragma unroll
+            for (int i = 0; i < 7; ++i) key[i] = key[i + 1];
+            key[7] = KEY_OUT;
+        }
+    }
+    again |= sub < a.k && near(mine, behind);
+    if (__any(valid && again)) choose64<LPT, BIAS>(a, row, bias, valid, here, e0, g, sub, s_choice);
+    __builtin_amdgcn_wave_barrier();
+    // the token's choices and weights: lane j has the j-th
+    const int id = sub < a.k && valid ? s_choice[sub] : -1;
+    const float x = id >= 0 ? row[id] : -INFINITY;
+    // renormalised scores, scaled so that the largest is near 1: exp(x - most), or 1 / (e^-M + e^(-x - M)) with M = max(0, -most)
+    float s = 0.0f, c = a.scale;
+    if (a.renormalise) {
+        const float most = token_max<LPT>(x), m = fmaxf(0.0f, -most);
+        if (!(x == -INFINITY || (sigmoid && x < LOGISTIC_ZERO)))
+            s = sigmoid ? __builtin_amdgcn_rcpf(__expf(-m) + __expf(-x - m)) : __expf(x - most);
+        const float sum = token_sum<LPT>(s);
+        c = sum == 0.0f ? 0.0f : a.scale * __builtin_amdgcn_rcpf(sum);
+    } else if (!(x == -INFINITY || (sigmoid && x < LOGISTIC_ZERO))) {
+        s = score(x);
+    }
+    if (in && sub < a.k) {
+        expert_idx[(size_t)t * a.k + sub] = id;
+        gate_w[(size_t)t * a.k + sub] = s * c;
     }
 }
 
 // ---------------------------------------------------------------------------
-// backward: a wave per token, four consecutive experts per lane
+// backward: LPT lanes per token, four consecutive experts each; lane j < k works out q_j
 // ---------------------------------------------------------------------------
+template <int LPT>
 __global__ __launch_bounds__(256) void router_bwd_kernel(const RouterArgs a, const float* __restrict__ logits,
                                                          const int32_t* __restrict__ expert_idx,
                                                          const float* __restrict__ dgate_w, float* __restrict__ dlogits) {
-    const int lane = threadIdx.x & 63, t = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (t >= a.T) return;
-    const bool sigmoid = a.score == MOE_SIGMOID;
-    const float* row = logits + (size_t)t * a.E;
-    int id[ROUTER_MAX_K];
-    float cl[ROUTER_MAX_K], dw[ROUTER_MAX_K], most = -INFINITY;
-    bool any = false;
-#pragma unroll
-    for (int j = 0; j < ROUTER_MAX_K; ++j) {
-        id[j] = j < a.k ? expert_idx[(size_t)t * a.k + j] : -1;
-        const bool ok = (unsigned)id[j] < (unsigned)a.E;
-        any |= ok;
-        cl[j] = ok ? row[id[j]] : -INFINITY;
-        dw[j] = ok ? dgate_w[(size_t)t * a.k + j] : 0.0f;
-        most = fmaxf(most, cl[j]);
+    const int lane = threadIdx.x & 63, sub = threadIdx.x & (LPT - 1), base = lane & ~(LPT - 1);
+    const int t = blockIdx.x * (256 / LPT) + threadIdx.x / LPT, e4 = 4 * sub;
+    const bool in = t < a.T, sigmoid = a.score == MOE_SIGMOID;
+    const float* row = logits + (size_t)(in ? t : 0) * a.E;
+    int id = in && sub < a.k ? expert_idx[(size_t)t * a.k + sub] : -1;
+    if ((unsigned)id >= (unsigned)a.E) id = -1;
+    float x = -INFINITY, dw = 0.0f;
+    if (id >= 0) {
+        x = row[id];
+        dw = dgate_w[(size_t)t * a.k + sub];
     }
-    float out[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (any) {
-        float r[ROUTER_MAX_K], q[ROUTER_MAX_K], sum = 0.0f, all = 0.0f, top = 0.0f, inv = 1.0f;
-        float l[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        const bool dense = !sigmoid && !a.renormalise;
-        if (dense) {
-            top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (4 * lane + i < a.E) l[i] = row[4 * lane + i];
-                top = fmaxf(top, l[i]);
-            }
-            top = wave_max(top);
-            if (top == -INFINITY) top = 0.0f;
-            float total = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) total += expf(l[i] - top);
-            total = wave_sum(total);
-            inv = total > 0.0f ? 1.0f / total : 0.0f;
-        }
-        const float m = a.renormalise ? fmaxf(0.0f, -most) : 0.0f, em = expf(-m);
-#pragma unroll
-        for (int j = 0; j < ROUTER_MAX_K; ++j) {
-            if (cl[j] == -INFINITY || (sigmoid && cl[j] < LOGISTIC_ZERO)) r[j] = 0.0f;
-            else if (sigmoid) r[j] = 1.0f / (em + expf(-cl[j] - m));
-            else r[j] = a.renormalise ? expf(cl[j] - most) : expf(cl[j] - top) * inv;
-            sum += r[j];
-        }
-        float mean = 0.0f;
-        if (a.renormalise) {
-            const float c = sum > 0.0f ? 1.0f / sum : 0.0f;
-#pragma unroll
-            for (int j = 0; j < ROUTER_MAX_K; ++j) {
-                r[j] *= c;
-                mean = fmaf(dw[j], r[j], mean);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < ROUTER_MAX_K; ++j) {
-            q[j] = a.scale * r[j] * (dw[j] - mean);
-            all += q[j];
-            if (sigmoid) q[j] *= 1.0f / (1.0f + expf(cl[j]));
+    float out[4] = {0.0f, 0.0f, 0.0f, 0.0f}, l[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    const bool vec = (a.E & 3) == 0, dense = !sigmoid && !a.renormalise;    // (the renormalised softmax's q sum to 0)
+    const bool none = x == -INFINITY || (sigmoid && x < LOGISTIC_ZERO);
+    float r = 0.0f, top = 0.0f, inv = 1.0f, mean = 0.0f;
+    if (dense) {
+        if (in) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (id[j] == 4 * lane + i) out[i] += q[j];
+                if (e4 + i < a.E) l[i] = row[e4 + i];
         }
-        if (dense) {
+        top = token_max<LPT>(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])));
+        if (top == -INFINITY) top = 0.0f;
+        float total = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) out[i] -= expf(l[i] - top) * inv * all;
-        }
+        for (int i = 0; i < 4; ++i) total += __expf(l[i] - top);
+        total = token_sum<LPT>(total);
+        inv = total > 0.0f ? 1.0f / total : 0.0f;
+        if (!none) r = __expf(x - top) * inv;
+    } else if (a.renormalise) {
+        const float most = token_max<LPT>(x), m = fmaxf(0.0f, -most);
+        if (!none) r = sigmoid ? __builtin_amdgcn_rcpf(__expf(-m) + __expf(-x - m)) : __expf(x - most);
+        const float sum = token_sum<LPT>(r);
+        r *= sum > 0.0f ? __builtin_amdgcn_rcpf(sum) : 0.0f;
+        mean = token_sum<LPT>(dw * r);
+    } else if (!none) {
+        r = __builtin_amdgcn_rcpf(1.0f + __expf(-x));
     }
-    float* o = dlogits + (size_t)t * a.E;
+    float q = none ? 0.0f : a.scale * r * (dw - mean);
+    const float all = dense ? token_sum<LPT>(q) : 0.0f;
+    if (sigmoid && !none) q *= __builtin_amdgcn_rcpf(1.0f + __expf(x));
+    for (int j = 0; j < a.k; ++j) {
+        const int ij = __shfl(id, base + j, MOE_WAVE) - e4;
+        const float qj = __shfl(q, base + j, MOE_WAVE);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (4 * lane + i < a.E) o[4 * lane + i] = out[i];
+        for (int i = 0; i < 4; ++i) out[i] += ij == i ? qj : 0.0f;
+    }
+    if (dense && all != 0.0f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] -= __expf(l[i] - top) * inv * all;
+    }
+    if (!in) return;
+    float* o = dlogits + (size_t)t * a.E;
+    if (vec) {
+        if (e4 < a.E) *reinterpret_cast<float4*>(o + e4) = make_float4(out[0], out[1], out[2], out[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (e4 + i < a.E) o[e4 + i] = out[i];
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -265,19 +374,15 @@ extern "C" int moe_router_fwd(const moe_router* router, const float* logits, con
     const moe_router& r = *router;
     RouterArgs a = {r.T, r.E, r.k, r.score, r.n_groups, r.E / r.n_groups, r.top_groups, r.group_best, r.renormalise != 0,
                     r.scale, 0, 0};
-    // four experts per lane where the groups' lanes, rounded up to powers of two, then fit in a wave; else eight, which
-    // always do (a group of S > 8 experts takes fewer than S / 4 lanes)
-    int Q = 4;
-    for (;; Q = 8) {
-        a.lg_log2 = log2_up(ceil_div(a.group, Q));
-        a.lpt_log2 = a.lg_log2 + log2_up(a.n_groups);
-        if (a.lpt_log2 <= 6 || Q == 8) break;
-    }
-    const int grid = ceil_div(r.T, 256 >> a.lpt_log2);
+    // the groups' lanes, rounded up to powers of two, always fit in a wave: of at most 256 experts, a group of S > 8 has fewer
+    // than S / 4 lanes
+    a.lg_log2 = log2_up(ceil_div(a.group, 8));
+    a.vec = a.group % 8 == 0 && (((uintptr_t)logits | (uintptr_t)select_bias_or_null) & 15) == 0;
+    const int lanes = a.lg_log2 + log2_up(r.n_groups);
     hipStream_t st = (hipStream_t)stream;
-#define FWD(Q, V) router_fwd_kernel<Q, V><<<grid, 256, 0, st>>>(a, logits, select_bias_or_null, token_mask_or_null, expert_idx, gate_w)
-    if (Q == 4) { if (select_bias_or_null) FWD(4, double); else FWD(4, float); }
-    else { if (select_bias_or_null) FWD(8, double); else FWD(8, float); }
+#define FWD(LPT) (select_bias_or_null ? router_fwd_kernel<LPT, true> : router_fwd_kernel<LPT, false>)<<<ceil_div(r.T, 256 / LPT), 256, 0, st>>>( \
+    a, logits, select_bias_or_null, token_mask_or_null, expert_idx, gate_w)
+    if (lanes <= 3) FWD(8); else if (lanes == 4) FWD(16); else if (lanes == 5) FWD(32); else FWD(64);
 #undef FWD
     return launch_status();
 }
@@ -290,7 +395,11 @@ extern "C" int moe_router_bwd(const moe_router* router, const float* logits, con
     const moe_router& r = *router;
     const RouterArgs a = {r.T, r.E, r.k, r.score, r.n_groups, r.E / r.n_groups, r.top_groups, r.group_best, r.renormalise != 0,
                           r.scale, 0, 0};
-    router_bwd_kernel<<<ceil_div(r.T, 4), 256, 0, (hipStream_t)stream>>>(a, logits, expert_idx, dgate_w, dlogits);
+    const int lanes = log2_up(ceil_div(r.E, 4));
+    hipStream_t st = (hipStream_t)stream;
+#define BWD(LPT) router_bwd_kernel<LPT><<<ceil_div(r.T, 256 / LPT), 256, 0, st>>>(a, logits, expert_idx, dgate_w, dlogits)
+    if (lanes <= 3) BWD(8); else if (lanes == 4) BWD(16); else if (lanes == 5) BWD(32); else BWD(64);
+#undef BWD
     return launch_status();
 }
 

@@ -91,6 +91,16 @@ def test_values(kind, score, bias):
             check(B.make_router(60, E, 6, score, groups, top, best, renorm, 1.0), 3, bias, kind, pad=0.2)
 
 
+def test_inputs_that_start_anywhere():
+    r = B.make_router(33, 64, 6, B.SIGMOID, 8, 3, 2)
+    l, b, m = inputs(r, 4, True, pad=0.3)
+    want = forward(r, l, b, m)
+    off = lambda t, n: torch.cat([torch.zeros(n, dtype=t.dtype), t.reshape(-1)]).cuda()[n:].reshape(t.shape)
+    for i, j in ((1, 0), (0, 3), (2, 2)):
+        got = forward(r, off(l, i), off(b, j), off(m, 1))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_near_ties_are_decided_in_64_bits():
     """Two experts whose score + bias differ by less than fp32 can tell, in every order."""
     T, E = 256, 32
