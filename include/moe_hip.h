@@ -533,7 +533,7 @@ int moe_layer_fwd_fp8(const moe_fp8_shape* shape, const moe_router* router, int3
 typedef struct {
     const void* grad;
     void* out;              /* not used by moe_grad_norm */
-    int64_t n;              /* elements, >= 0 */
+    int64_t n;              /* elements, 0 .. 2^43 (else MOE_ERR_SHAPE) */
     int32_t dtype;          /* moe_dtype */
 } moe_grad;
 size_t moe_grad_workspace_bytes(const moe_grad* grads, int32_t count);

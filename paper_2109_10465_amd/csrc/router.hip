@@ -505,6 +505,84 @@ __global__ __launch_bounds__(SORT_CHUNK) void sort_place_kernel(int n, int E, co
     row_of[i] = row;
 }
 
+// All of it in one workgroup, for few choices: three dependent launches of which none has work for the chip.  The choices
+// are counted, then placed in rounds of one per thread.
+#define SORT_SMALL 8192
+__global__ __launch_bounds__(SORT_CHUNK) void sort_small_kernel(int n, int E, const int32_t* __restrict__ expert_idx,
+                                                                int32_t* __restrict__ row_of,
+                                                                int32_t* __restrict__ expert_start) {
+    constexpr int WAVES = SORT_CHUNK / 64, ROUNDS = SORT_SMALL / SORT_CHUNK;
+    __shared__ int s_next[256];                 // the next choice's row of an expert
+    __shared__ int16_t s_cnt[WAVES][256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int e[ROUNDS];
+    if (threadIdx.x < 256) s_next[threadIdx.x] = 0;
+    for (int x = threadIdx.x; x < WAVES * 256 / 2; x += SORT_CHUNK) reinterpret_cast<int*>(s_cnt)[x] = 0;
+#pragma unroll
+    for (int u = 0; u < ROUNDS; ++u) {
+        const int i = u * SORT_CHUNK + threadIdx.x;
+        e[u] = i < n ? expert_idx[i] : -1;
+        if ((unsigned)e[u] >= (unsigned)E) e[u] = -1;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < ROUNDS; ++u)
+        if (e[u] >= 0) atomicAdd(&s_next[e[u]], 1);
+    __syncthreads();
+    if (wave == 0) {                            // four experts per lane
+        int v[4], sum = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            v[q] = s_next[4 * lane + q];
+            sum += v[q];
+        }
+        int run = scan_up(sum, lane) - sum;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int x = 4 * lane + q;
+            s_next[x] = run;
+            if (x < E) expert_start[x] = run;
+            run += v[q];
+            if (x == E - 1) expert_start[E] = run;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < ROUNDS; ++u) {
+        if (u * SORT_CHUNK >= n) break;         // uniform
+        const int i = u * SORT_CHUNK + threadIdx.x;
+        const bool ok = e[u] >= 0;
+        unsigned long long same = __ballot(ok);
+#pragma unroll
+        for (int b = 0; b < 8; ++b) {
+            const bool bit = e[u] >> b & 1;
+            const unsigned long long m = __ballot(ok && bit);
+            same &= bit ? m : ~m;
+        }
+        const int rank = __popcll(same & ((1ull << lane) - 1ull));
+        if (ok && rank == 0) s_cnt[wave][e[u]] = (int16_t)__popcll(same);
+        __syncthreads();
+        int row = -1;
+        if (ok) {
+            row = s_next[e[u]] + rank;
+            for (int w = 0; w < wave; ++w) row += s_cnt[w][e[u]];
+        }
+        if (i < n) row_of[i] = row;
+        if ((u + 1) * SORT_CHUNK >= n) break;   // uniform
+        __syncthreads();
+        if (threadIdx.x < 256) {                // the round's counts move on, and are cleared
+            int sum = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                sum += s_cnt[w][threadIdx.x];
+                s_cnt[w][threadIdx.x] = 0;
+            }
+            s_next[threadIdx.x] += sum;
+        }
+        __syncthreads();
+    }
+}
+
 int sort_check(const moe_router* r, const int32_t* expert_idx, const int32_t* row_of, const int32_t* expert_start,
                const void* ws, size_t ws_bytes) {
     const int rc = router_status(r);
@@ -525,6 +603,10 @@ extern "C" int moe_sort_choices(const moe_router* router, const int32_t* expert_
     int32_t* hist = (int32_t*)ws;
     int32_t* total = (int32_t*)((char*)ws + align_up((size_t)chunks * E * 4, 256));
     hipStream_t st = (hipStream_t)stream;
+    if (n <= SORT_SMALL) {
+        sort_small_kernel<<<1, SORT_CHUNK, 0, st>>>(n, E, expert_idx, row_of, expert_start);
+        return launch_status();
+    }
     sort_count_kernel<<<chunks, SORT_CHUNK, 0, st>>>(n, E, expert_idx, hist);
     sort_scan_kernel<<<E, 64, 0, st>>>(chunks, E, hist, total);
     sort_place_kernel<<<chunks, SORT_CHUNK, 0, st>>>(n, E, expert_idx, hist, total, row_of, expert_start);

@@ -154,7 +154,7 @@ def test_non_finite_logits_give_indices_in_range():
         assert all(len(set(row.tolist())) == 8 for row in i)
 
 
-@pytest.mark.parametrize("T,k,E", [(1, 1, 1), (1, 8, 256), (5, 3, 7), (64, 2, 4), (1023, 1, 256), (1025, 1, 3), (4000, 8, 60),
+@pytest.mark.parametrize("T,k,E", [(1, 1, 1), (1, 8, 256), (5, 3, 7), (64, 2, 4), (1023, 1, 256), (1025, 1, 3), (1024, 8, 256), (1025, 8, 256), (700, 4, 90), (4000, 8, 60),
                                    (9001, 7, 200), (70000, 2, 256)])
 @pytest.mark.parametrize("kind", ["even", "one", "some"])
 def test_sort(T, k, E, kind):
