@@ -488,7 +488,8 @@ int moe_dispatch_fp8(const moe_fp8_shape* shape, const void* x, const int32_t* r
                      uint8_t* xb, void* stream);
 
 /* The experts' block: h = act(x W1) in 8 bits -> hq[R,Kp(d_ff)], hb;  yd[R,d_model] = h W2, of type
- * yd_dtype.  The hidden activation is formed in fp32 and rounded once, to the format above. */
+ * yd_dtype.  The hidden activation is formed in fp32 and rounded once, to the format
+ * above (with exponents not below -126, and NaN passed over in finding them). */
 int moe_expert_ffn_fwd_fp8(const moe_fp8_shape* shape, const void* xq, const uint8_t* xb,
                            const int32_t* expert_start, const void* W1q, const uint8_t* W1b,
                            const void* W2q, const uint8_t* W2b, void* hq, uint8_t* hb, int32_t yd_dtype,

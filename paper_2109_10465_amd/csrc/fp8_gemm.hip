@@ -10,6 +10,7 @@
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short i16x2_t __attribute__((ext_vector_type(2)));
 
 struct Fp8Args {
     const uint8_t *xq, *xb, *wq, *wb;
@@ -69,15 +70,17 @@ __device__ __forceinline__ float activate(f32x16_t& v, float top) {
     }
     return top;
 }
-// g: the reciprocal of the block's unit (8-bit output)
+// unit: the block's, a power of two (8-bit output); the conversion divides by it
 template <int OUT>
-__device__ __forceinline__ void store_tile(const Fp8Args& p, const f32x16_t& v, int nb, int f, int r, bool live, int half, float g) {
+__device__ __forceinline__ void store_tile(const Fp8Args& p, const f32x16_t& v, int nb, int f, int r, bool live, int half, float unit) {
     if constexpr (OUT == OUT_RELU8 || OUT == OUT_GELU8) {
         uint32_t d[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * q] * g, v[4 * q + 1] * g, 0, false);
-            d[q] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * q + 2] * g, v[4 * q + 3] * g, w, true);
+            i16x2_t w = {0, 0};
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[4 * q], v[4 * q + 1], unit, false);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[4 * q + 2], v[4 * q + 3], unit, true);
+            d[q] = __builtin_bit_cast(uint32_t, w);
         }
         swap_halves(d[0], d[2]);
         swap_halves(d[1], d[3]);
@@ -116,17 +119,18 @@ __device__ __forceinline__ void store_byte(const Fp8Args& p, int byte, int nb, i
 // all four tiles of a block in one wave
 template <int OUT>
 __device__ __forceinline__ void store_block(const Fp8Args& p, f32x16_t (&acc)[4], int nb, int r, bool live, int half) {
-    float g = 0.0f;
+    float unit = 1.0f;
     if constexpr (OUT == OUT_RELU8 || OUT == OUT_GELU8) {
         float top = 0.0f;
 #pragma unroll
         for (int f = 0; f < 4; ++f) top = activate<OUT>(acc[f], top);
-        const int byte = scale_byte(__float_as_uint(fmaxf(top, __shfl_xor(top, 32, MOE_WAVE))));
-        g = scale_inverse(byte);
+        // (a unit that fp32 holds as a normal number: 2^-126 at least)
+        const int byte = max(1, scale_byte(__float_as_uint(fmaxf(top, __shfl_xor(top, 32, MOE_WAVE)))));
+        unit = __uint_as_float((uint32_t)byte << 23);
         if (live) store_byte(p, byte, nb, r, half);
     }
 #pragma unroll
-    for (int f = 0; f < 4; ++f) store_tile<OUT>(p, acc[f], nb, f, r, live, half, g);
+    for (int f = 0; f < 4; ++f) store_tile<OUT>(p, acc[f], nb, f, r, live, half, unit);
 }
 
 // Which expert and rows the row tile `at` has, tiles of TR rows, expert by expert: found by a wave, four experts a lane
@@ -283,7 +287,7 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
     int* tiles = reinterpret_cast<int*>(smem + G::TABLE);
     int* start = tiles + 260;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int l32 = lane & 31, half = lane >> 5, wf = wave / WT, wt = wave % WT;
+    const int l32 = lane & 31, half = lane >> 5, wf = wave % WF, wt = wave / WF;     // (waves without rows are then spread over the SIMDs)
     const int ctiles = (p.nnb + WF - 1) / WF;
     if (wave == 0) {
         int s[5], t[4], n = 0;
@@ -395,6 +399,9 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
                 for (int i = 0; i < 16; ++i) acc[t][f][i] = 0.0f;
         int we = 0, xe[TT] = {};
         bool again = false;
+        // a wave without rows (or columns) only helps to load: its products would cost the time of the others' and power, which
+        // is what limits the clock
+        const bool live = cur.row + wt * TT * 32 < cur.end && cur.col + wf < p.nnb;
         Fp8Place after = cur;
         for (int kb = 0; kb < p.nkb; ++kb, stage ^= 1) {
             // this slab has arrived, and every wave is done with the one before
@@ -406,26 +413,28 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
             }
             if (kb + 1 == p.nkb) { after = next; again = more; }
             if (more) fetch(stage ^ 1);
-            const uint8_t* w = smem + stage * G::STAGE + wbase;
-            const uint8_t* x = smem + stage * G::STAGE + xbase;
+            if (live) {
+                const uint8_t* w = smem + stage * G::STAGE + wbase;
+                const uint8_t* x = smem + stage * G::STAGE + xbase;
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                i32x8_t b[TT];
+                for (int s = 0; s < 2; ++s) {
+                    i32x8_t b[TT];
 #pragma unroll
-                for (int t = 0; t < TT; ++t)
-                    b[t] = two16(*reinterpret_cast<const uint4*>(x + t * 4096 + frag[2 * s]), *reinterpret_cast<const uint4*>(x + t * 4096 + frag[2 * s + 1]));
+                    for (int t = 0; t < TT; ++t)
+                        b[t] = two16(*reinterpret_cast<const uint4*>(x + t * 4096 + frag[2 * s]), *reinterpret_cast<const uint4*>(x + t * 4096 + frag[2 * s + 1]));
 #pragma unroll
-                for (int f = 0; f < 4; ++f) {
-                    const i32x8_t a = two16(*reinterpret_cast<const uint4*>(w + f * 4096 + frag[2 * s]), *reinterpret_cast<const uint4*>(w + f * 4096 + frag[2 * s + 1]));
+                    for (int f = 0; f < 4; ++f) {
+                        const i32x8_t a = two16(*reinterpret_cast<const uint4*>(w + f * 4096 + frag[2 * s]), *reinterpret_cast<const uint4*>(w + f * 4096 + frag[2 * s + 1]));
 #pragma unroll
-                    for (int t = 0; t < TT; ++t) acc[t][f] = mma<0>(a, b[t], acc[t][f], we, xe[t]);
+                        for (int t = 0; t < TT; ++t) acc[t][f] = mma<0>(a, b[t], acc[t][f], we, xe[t]);
+                    }
                 }
             }
             we = (int)((uint32_t)we >> 8);
 #pragma unroll
             for (int t = 0; t < TT; ++t) xe[t] = (int)((uint32_t)xe[t] >> 8);
         }
-        if (cur.col + wf < p.nnb) {
+        if (live) {
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
                 const int r = cur.row + (wt * TT + t) * 32 + l32;
