@@ -51,7 +51,7 @@ int moe_expert_ffn_parts(const moe_shape* shape, int32_t* parts);
 int moe_expert_ffn_direct(const moe_shape* shape, int32_t* direct, int32_t* workgroups);
 
 /* Kernels of moe_expert_ffn_fwd_fp8's two products: 0 = tiles of 256 x 256, 1 = of 128 x 128, 2 = of 32 x 32 with a split
- * reduction (second product only). */
+ * reduction (second product only), 3 = of 128 columns x 64 rows. */
 int moe_fp8_kernels(const moe_fp8_shape* shape, int32_t* first, int32_t* second);
 
 #ifdef __cplusplus

@@ -241,19 +241,24 @@ __global__ __launch_bounds__(64 * THIN8_WAVES, 2) void fp8_thin_kernel(const Fp8
 // ---------------------------------------------------------------------------
 // tiles staged through LDS
 // ---------------------------------------------------------------------------
-// WF x WT waves; a wave has 128 columns and 32 TT rows, four by TT matrix tiles of 32 x 32.  A slab is 128 reduction
-// entries of the tile's columns and rows; two slabs are in LDS, the next one being filled by loads that write LDS
-// themselves.  A workgroup walks its tiles and treats their slabs as one stream, so the next tile's first slab is on
-// its way during a tile's epilogue.
-template <int WF, int WT, int TT>
+// WF x WT waves; a wave has 128 columns and 32 TT rows, four by TT matrix tiles of 32 x 32.  A tile has BT rows: those of all
+// waves, or only the first one's (then the others help to load).  A slab is 128 reduction entries of the tile's columns and
+// rows; NS slabs have a place in LDS, one is worked on, the others are being filled by loads that write LDS themselves.  A
+// workgroup walks its tiles and treats their slabs as one stream, so the next tile's first slabs are on their way during a
+// tile's epilogue.
+template <int WF, int WT, int TT, int BT_, int NS_>
 struct Fp8Tile {
-    static constexpr int NW = WF * WT, NT = 64 * NW;
-    static constexpr int BF = 128 * WF, BT = 32 * TT * WT;          // columns and rows
+    static constexpr int NW = WF * WT, NT = 64 * NW, NS = NS_;
+    static constexpr int BF = 128 * WF, BT = BT_;                   // columns and rows
     static constexpr int STAGE = (BF + BT) * 128;
     static constexpr int WL = BF / 8 / NW, XL = BT / 8 / NW;        // loads of a slab per wave: 8 rows of 128 bytes each
-    static constexpr int TABLE = 2 * STAGE;                         // running tile counts and starts behind the stages
-    static constexpr int BYTES = TABLE + (260 + 260) * 4;
+    static constexpr int TABLE = NS * STAGE;                        // running tile counts and starts behind the stages
+    static constexpr int EXPS = TABLE + (260 + 260) * 4;            // then, per wave, two buffers of exponent words:
+    static constexpr int XW = (TT + 1) / 2;                         // XW loads of 64 rows' ones and one of the columns'
+    static constexpr int BYTES = EXPS + NW * 2 * (XW + 1) * 256;
     static_assert(BF % (8 * NW) == 0 && BT % (8 * NW) == 0 && NW % 2 == 0, "whole loads per wave");
+    static_assert((NS - 2) * (WL + XL) < 64, "vmcnt is a 6-bit counter");
+    static_assert(NS == 2 || NS == 3, "two buffers of exponents");
 };
 
 #define FP8_BAND 4      // row tiles per band of the walk inside an expert: an XCD's workgroups share 4 row panels at a time
@@ -280,9 +285,9 @@ __device__ __forceinline__ Fp8Place fp8_place(const int* tiles, const int* start
             __builtin_amdgcn_readfirstlane(col * WF)};
 }
 
-template <int WF, int WT, int TT, int OUT>
+template <int WF, int WT, int TT, int BT, int NS, int OUT>
 __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args p) {
-    typedef Fp8Tile<WF, WT, TT> G;
+    typedef Fp8Tile<WF, WT, TT, BT, NS> G;
     extern __shared__ __align__(1024) uint8_t smem[];
     int* tiles = reinterpret_cast<int*>(smem + G::TABLE);
     int* start = tiles + 260;
@@ -315,10 +320,11 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
     }
     __syncthreads();
     const int total = __builtin_amdgcn_readfirstlane(tiles[256]);
-    // workgroup w is on XCD w % 8; an XCD takes as many consecutive tiles at a time as it has workgroups
-    const int per = gridDim.x >> 3, xcd = blockIdx.x & 7;
+    // workgroup w is on XCD w % 8; an XCD takes as many consecutive tiles at a time as it has workgroups, or an eighth of
+    // them where there are fewer: the grid holds for any distribution of the rows
+    const int per = min((int)gridDim.x >> 3, (total + 7) >> 3), xcd = blockIdx.x & 7;
     int at = xcd * per + (blockIdx.x >> 3);
-    if (at >= total) return;
+    if ((int)(blockIdx.x >> 3) >= per || at >= total) return;
     const int stride = per * 8;
     const uint32_t kbytes = (uint32_t)p.nkb * 128;
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)smem;
@@ -336,59 +342,67 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
     for (int c = 0; c < 4; ++c) frag[c] = l32 * 128 + (((4 * (c >> 1) + 2 * half + (c & 1)) ^ ((l32 >> 1) & 7)) << 4);
     const uint32_t wbase = wf * 128 * 128, xbase = G::BF * 128 + wt * TT * 32 * 128;
 
-    // the cursor of the loads, one slab ahead of the products
+    auto scalar = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
+    auto desc = [&](uint64_t base, uint64_t n) {
+        return u32x4_buf_t{scalar((uint32_t)base), scalar((uint32_t)(base >> 32) & 0xffffu), scalar(n < 0x7fffffffull ? (uint32_t)n : 0x7fffffffu), 0x00020000u};
+    };
+    auto load_word = [](u32x4_buf_t d, uint32_t off, uint32_t to) {         // 64 lanes' words, one after the other
+        asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(to), "v"(off), "s"(d) : "memory");
+    };
+    // the cursor of the loads, NS - 1 slabs ahead of the products: the tile, its slab, and what is left of its operands
     Fp8Place next = fp8_place<G::BT, WF>(tiles, start, at, ctiles, lane);
-    int nkb = 0;                        // its slab
+    int nkb = 0, group = 0;             // group: which buffer takes the exponents of the next four slabs
     bool more = true;
     u32x4_buf_t wd, xd;
-    int we_next = 0, xe_next[TT];
-    auto scalar = [](u32x4_buf_t d) {       // (the compiler does not see that a whole wave has the same ones)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) d[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)d[i]);
-        return d;
-    };
     auto aim = [&]() {
-        const uint32_t wleft = (uint32_t)(p.nnb - next.col) * 128 * kbytes;
-        wd = make_desc(p.wq + ((size_t)next.e * p.nnb + next.col) * 128 * kbytes, wleft);
-        const size_t xleft = (size_t)(next.end - next.row) * kbytes;
-        xd = make_desc(p.xq + (size_t)next.row * kbytes, xleft < 0x7fffffffull ? (uint32_t)xleft : 0x7fffffffu);
+        wd = desc((uint64_t)(p.wq + ((size_t)next.e * p.nnb + next.col) * 128 * kbytes), (uint64_t)(p.nnb - next.col) * 128 * kbytes);
+        xd = desc((uint64_t)(p.xq + (size_t)next.row * kbytes), (uint64_t)(next.end - next.row) * kbytes);
     };
+    auto step = [&](u32x4_buf_t& d) {   // 128 bytes further, and as much less to the end
+        const uint32_t lo = d[0] + 128;
+        d[1] = scalar(d[1] + (lo < 128 ? 1 : 0));
+        d[0] = scalar(lo);
+        d[2] = scalar(d[2] > 128 ? d[2] - 128 : 0);
+    };
+    const uint32_t exps = lds + G::EXPS + wave * 2 * (G::XW + 1) * 256;
+    // Past the last tile the requests go on, for nothing (an empty range), so that a wait can count on their number.
     auto fetch = [&](int stage) {
-        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + stage * G::STAGE);
-        const u32x4_buf_t wdesc = scalar(wd), xdesc = scalar(xd);
         if ((nkb & 3) == 0) {
             const int nb = min(next.col + wf, p.nnb - 1);
-            we_next = *reinterpret_cast<const int*>(p.wb + ((size_t)next.e * p.nnb + nb) * p.xb_stride + nkb);
+            const uint32_t to = scalar(exps + group * (G::XW + 1) * 256);
+            group ^= 1;
+            const u32x4_buf_t ed = desc((uint64_t)(p.xb + (size_t)next.row * p.xb_stride + nkb),
+                                        more ? (uint64_t)min(next.end - next.row, G::BT) * p.xb_stride - nkb : 0);
 #pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                const int r = min(next.row + (wt * TT + t) * 32 + l32, next.end - 1);
-                xe_next[t] = *reinterpret_cast<const int*>(p.xb + (size_t)r * p.xb_stride + nkb);
-            }
+            for (int i = 0; i < G::XW; ++i) load_word(ed, (uint32_t)(wt * TT * 32 + 64 * i + lane) * p.xb_stride, to + 256 * i);
+            load_word(desc((uint64_t)(p.wb + ((size_t)next.e * p.nnb + nb) * p.xb_stride + nkb), more ? 4 : 0), 0, to + 256 * G::XW);
         }
+        const uint32_t to = scalar(lds + stage * G::STAGE);
 #pragma unroll
-        for (int i = 0; i < G::WL; ++i) load_to_lds(wdesc, voff[i], to + (i * G::NW + wave) * 1024);
+        for (int i = 0; i < G::WL; ++i) load_to_lds(wd, voff[i], to + (i * G::NW + wave) * 1024);
 #pragma unroll
-        for (int i = 0; i < G::XL; ++i) load_to_lds(xdesc, voff[i], to + G::BF * 128 + (i * G::NW + wave) * 1024);
-        if (++nkb == p.nkb) {
+        for (int i = 0; i < G::XL; ++i) load_to_lds(xd, voff[i], to + G::BF * 128 + (i * G::NW + wave) * 1024);
+        if (++nkb < p.nkb) {
+            step(wd);
+            step(xd);
+        } else {
             nkb = 0;
             at += stride;
-            more = at < total;
+            more = more && at < total;
             if (more) {
                 next = fp8_place<G::BT, WF>(tiles, start, at, ctiles, lane);
                 aim();
+            } else {
+                wd[2] = xd[2] = 0;
             }
-        } else {
-            // the next slab: 128 bytes further, and as much less to the end
-            uint64_t a = ((uint64_t)wd[1] << 32 | wd[0]) + 128;
-            wd[0] = (uint32_t)a; wd[1] = (uint32_t)(a >> 32); wd[2] = wd[2] > 128 ? wd[2] - 128 : 0;
-            a = ((uint64_t)xd[1] << 32 | xd[0]) + 128;
-            xd[0] = (uint32_t)a; xd[1] = (uint32_t)(a >> 32); xd[2] = xd[2] > 128 ? xd[2] - 128 : 0;
         }
     };
     aim();
     Fp8Place cur = next;
-    fetch(0);
-    int stage = 0;
+    int cat = at;                       // the products' tile
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) fetch(s);
+    int stage = 0, have = 0;
     for (;;) {
         f32x16_t acc[TT][4];
 #pragma unroll
@@ -398,21 +412,23 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[t][f][i] = 0.0f;
         int we = 0, xe[TT] = {};
-        bool again = false;
         // a wave without rows (or columns) only helps to load: its products would cost the time of the others' and power, which
         // is what limits the clock
-        const bool live = cur.row + wt * TT * 32 < cur.end && cur.col + wf < p.nnb;
-        Fp8Place after = cur;
-        for (int kb = 0; kb < p.nkb; ++kb, stage ^= 1) {
-            // this slab has arrived, and every wave is done with the one before
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const bool live = wt * TT * 32 < G::BT && cur.row + wt * TT * 32 < cur.end && cur.col + wf < p.nnb;
+        for (int kb = 0; kb < p.nkb; ++kb) {
+            // this slab has arrived once at most the NS - 2 younger ones are outstanding, and every wave is done with the one
+            // before, whose place is filled again
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"((NS - 2) * (G::WL + G::XL)) : "memory");
             if ((kb & 3) == 0) {
-                we = we_next;
+                const int* e = reinterpret_cast<const int*>(smem + G::EXPS + (wave * 2 + have) * (G::XW + 1) * 256);
+                have ^= 1;
 #pragma unroll
-                for (int t = 0; t < TT; ++t) { xe[t] = xe_next[t]; asm volatile("" : "+v"(xe[t])); }
+                for (int t = 0; t < TT; ++t) xe[t] = e[32 * t + l32];
+                we = e[64 * G::XW];
+                // with three slabs in flight and a reduction of one, the next request is for this very buffer
+                if constexpr (NS > 2) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
-            if (kb + 1 == p.nkb) { after = next; again = more; }
-            if (more) fetch(stage ^ 1);
+            fetch(stage == 0 ? NS - 1 : stage - 1);
             if (live) {
                 const uint8_t* w = smem + stage * G::STAGE + wbase;
                 const uint8_t* x = smem + stage * G::STAGE + xbase;
@@ -433,6 +449,7 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
             we = (int)((uint32_t)we >> 8);
 #pragma unroll
             for (int t = 0; t < TT; ++t) xe[t] = (int)((uint32_t)xe[t] >> 8);
+            stage = stage == NS - 1 ? 0 : stage + 1;
         }
         if (live) {
 #pragma unroll
@@ -441,9 +458,11 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
                 store_block<OUT>(p, acc[t], cur.col + wf, r, r < cur.end, half);
             }
         }
-        if (!again) break;
-        cur = after;
+        cat += stride;
+        if (cat >= total) break;
+        cur = fp8_place<G::BT, WF>(tiles, start, cat, ctiles, lane);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the last requests write this workgroup's LDS
 }
 
 // compute units of the current device (looked up once per device)
@@ -460,11 +479,11 @@ static int compute_units() {
     return n;
 }
 
-template <int WF, int WT, int TT, int OUT>
+template <int WF, int WT, int TT, int BT, int NS, int OUT>
 static int launch_tiles(const Fp8Args& p, int per_cu, hipStream_t st) {
-    typedef Fp8Tile<WF, WT, TT> G;
+    typedef Fp8Tile<WF, WT, TT, BT, NS> G;
     static unsigned long long opted;
-    const auto kern = fp8_tile_kernel<WF, WT, TT, OUT>;
+    const auto kern = fp8_tile_kernel<WF, WT, TT, BT, NS, OUT>;
     if (!lds_opt_in((const void*)kern, G::BYTES, &opted)) return MOE_ERR_LAUNCH;
     const long long most = ((long long)p.rows / G::BT + (p.E < p.rows ? p.E : p.rows)) * ((p.nnb + WF - 1) / WF);
     long long wgs = (long long)compute_units() * per_cu / 8 * 8;
@@ -475,12 +494,16 @@ static int launch_tiles(const Fp8Args& p, int per_cu, hipStream_t st) {
 }
 
 // Which kernel?  Estimated from the mean rows of the experts that can have any.
-enum { FP8_LARGE = 0, FP8_SMALL = 1, FP8_THIN = 2 };
+enum { FP8_LARGE = 0, FP8_SMALL = 1, FP8_THIN = 2, FP8_NARROW = 3 };
 // 256 x 256 or 128 x 128: a CU holds one workgroup of the large tile, which works off its area a fifth faster (half the
 // operands per product), or two of the small one; either way the launch takes whole rounds of tiles.  Measured, large against
 // small, us: 131072 rows, 2048 x 8192, 16 experts: first product 2419, 2700, second 1849, 2187; 10006 rows, 776 x 3080, 6
 // experts with a Zipf gate: first 80, 64 (three rounds against four halves), second 46, 52; 4096 rows, 1024 x 4096,
 // 16 experts: first 34, 36, second (64 tiles) 53, 34.
+// 128 columns x 64 rows, three slabs in flight instead of two: where an expert's rows fit one tile either way, the weights'
+// bytes are the time, and more of them are on their way.  Narrow against small, us, both products of 32 experts, 1024 x 4096
+// (268 MB of weights): 122 rows 49.0, 59.2; 1024 rows 49.5, 62.2; 1536 rows 52.7, 63.3; 2048 rows 54.4, 64.2 dealt evenly, but
+// there a second row tile for half of the experts costs 30; 4096 rows 85.7, 73.4.
 // 32 x 32 with an eight-way split reduction: where there are so few small tiles that one tile's reduction is the launch's
 // time, 0.6 us for each of its 128 entries, against 0.084 us for each small tile's worth of thin ones.  8 rows of 8
 // experts, 1024 x 4096: second product 23.1 us with the small tile, 10.4 thin; 2048 x 2048: 13.3, 15.7; 122 rows of 32 experts,
@@ -489,6 +512,7 @@ static int fp8_kernel(int rows, int experts, int nkb, int nnb, bool hidden) {
     const long long E = experts < rows ? experts : rows, per = (rows + E - 1) / E, cus = compute_units();
     const long long large = E * ((per + 255) / 256) * ((nnb + 1) / 2), small = E * ((per + 127) / 128) * nnb;
     if (!hidden && per <= 32 && 7 * (long long)nkb > 15 + small) return FP8_THIN;
+    if (per <= 48) return FP8_NARROW;
     return 40 * ((large + cus - 1) / cus) < 24 * ((small + 2 * cus - 1) / (2 * cus)) ? FP8_LARGE : FP8_SMALL;
 }
 
@@ -503,7 +527,8 @@ static int launch_fp8(const Fp8Args& p, hipStream_t st) {
             return MOE_OK;
         }
     }
-    return kind == FP8_LARGE ? launch_tiles<2, 4, 2, OUT>(p, 1, st) : launch_tiles<1, 4, 1, OUT>(p, 2, st);
+    if (kind == FP8_NARROW) return launch_tiles<1, 4, 1, 64, 3, OUT>(p, 2, st);
+    return kind == FP8_LARGE ? launch_tiles<2, 4, 2, 256, 2, OUT>(p, 1, st) : launch_tiles<1, 4, 1, 128, 2, OUT>(p, 2, st);
 }
 
 // measurement aid: the kernels of the block's two products

@@ -136,7 +136,7 @@ def test_product(counts, K, N, dtype):
 
 @pytest.mark.parametrize("counts,K,N", [((700, 900, 300), 640, 776), ((4000,), 384, 256), ((40,) * 100, 256, 384), ((8,) * 256, 520, 128),
                                         ((2500, 100, 0, 1), 1024, 1032), ((4000,), 384, 4096), ((2500, 1200, 0, 700), 1160, 2056),
-                                        ((257,) * 64, 136, 1048)])
+                                        ((257,) * 64, 136, 1048), ((30, 0, 70, 64) * 64, 120, 1032), ((33,) * 200, 384, 1160)])
 def test_larger_products(counts, K, N):
     xq, xb, wq, wb = operands(counts, K, N, K + N)
     y = torch.empty((sum(counts), N), dtype=torch.bfloat16, device="cuda")
@@ -152,6 +152,7 @@ def test_every_kernel_is_reached_above():
     assert kinds((2500, 1200, 0, 700), 264, 2056)[0] == 0 and kinds((900, 700, 800), 256, 512) == (1, 1)
     # as products: K is the reduction, which is d_ff for the second
     assert kinds((4000,), 4096, 384)[1] == kinds((2500, 1200, 0, 700), 2056, 1160)[1] == 0
+    assert kinds((40,) * 100, 256, 384) == kinds((30, 0, 70, 64) * 64, 120, 1032) == kinds((33,) * 200, 384, 1160) == (3, 3)
     assert kinds((1,), 264, 2048)[1] == kinds((3, 0, 2, 3), 264, 1160)[1] == 2
 
 
