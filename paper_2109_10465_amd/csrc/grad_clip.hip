@@ -1,8 +1,10 @@
 // moe_grad_norm / moe_clip_grads: the global norm of many gradients, and clipping to it.
 //
 // The list of tensors travels in the kernels' arguments, a table of them per launch.  A launch's tensors are cut into parts,
-// which its workgroups take in turn; each leaves one sum of squares, in 64 bits, in the workspace.  Every workgroup of the
-// clipping launches adds those sums itself, in one order: that is a few KB of the L2 and saves a launch.  Squares are
+// which its workgroups take in turn; each leaves one sum of squares, in 64 bits, in the workspace.  Up to 2048 of them
+// are added by every workgroup of the clipping launch itself, in one order: that is 16 KB of the L2 and saves a launch (157
+// tensors of 2.2 M elements together 15.7 us, 22.5 with it).  More of them, from a second table on, are added once: each launch would read them
+// for every part (300 tensors of 2^20 floats 247 us, 268 otherwise; 1200 tensors 986, 1453).  Squares are
 // summed in 64 bits because gradients may be anything that fp32 holds: the square of 2e19 is beyond fp32, that of 1e-23
 // below it.  Bound: HBM; everything is read twice and written once.  270 M floats and 130 M bfloat16: squares 254 us (5.3
 // TB/s), clipping 505 (5.3).  The clipping pass has a workgroup for nearly every part: with 2048 that take parts in turn it is
@@ -13,6 +15,7 @@
 #define GRAD_TABLE 160          // tensors per launch: 24 bytes each, inside 4 KB of arguments
 #define GRAD_WGS 2048           // workgroups, and so sums, of a squares launch, at most: eight per CU
 #define GRAD_CLIP_WGS 65536     // of a clipping launch
+#define GRAD_SUMS 2048          // that each of a clipping launch's workgroups adds up itself, at most
 
 struct GradTable {
     const void* in[GRAD_TABLE];
@@ -98,6 +101,7 @@ __global__ __launch_bounds__(256) void grad_squares_kernel(const GradTable t, do
 // the norm, in every thread of the workgroup
 __device__ __forceinline__ float norm_of(int n, const double* __restrict__ sums) {
     double s = 0.0;
+#pragma unroll 8
     for (int i = threadIdx.x; i < n; i += 256) s += sums[i];
     return (float)sqrt(block_sum(s));
 }
@@ -123,9 +127,9 @@ __device__ __forceinline__ void scale_part(const T* p, T* o, int64_t a, int64_t 
 }
 
 __global__ __launch_bounds__(256) void grad_scale_kernel(const GradTable t, float max_norm, int n, const double* __restrict__ sums,
-                                                         float* __restrict__ norm) {
-    const float v = norm_of(n, sums);
-    if (blockIdx.x == 0 && threadIdx.x == 0) norm[0] = v;       // (every launch writes the same)
+                                                         float* norm) {
+    const float v = n ? norm_of(n, sums) : norm[0];
+    if (n && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = v;  // (every launch writes the same)
     const bool clip = v > max_norm && v < INFINITY;
     const float f = clip ? max_norm / v : 1.0f;
     for (int i = blockIdx.x; i < t.first[t.count]; i += gridDim.x) {
@@ -163,7 +167,7 @@ static void each_table(const moe_grad* g, int count, int most, F f) {
     for (int i = 0; i < count; ++i) {
         if (g[i].n == 0) continue;
         const int64_t parts = (g[i].n + t.part - 1) / t.part;
-        if (t.count == GRAD_TABLE || t.first[t.count] + parts >= (1ll << 31)) flush();
+        if (t.count == GRAD_TABLE || t.first[t.count] + parts > (1 << 30)) flush();
         t.in[t.count] = g[i].grad;
         t.out[t.count] = g[i].out;
         t.tail[t.count] = (int32_t)(g[i].n - (parts - 1) * t.part);
@@ -231,12 +235,10 @@ extern "C" int moe_clip_grads(const moe_grad* grads, int32_t count, float max_no
     if (!ws_ok(ws, ws_bytes, grad_ws_bytes(grads, count))) return MOE_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     const int n = squares_impl(grads, count, (double*)ws, st);
-    if (n == 0) {       // nothing but empty tensors
-        grad_norm_kernel<<<1, 256, 0, st>>>(0, (const double*)ws, norm);
-        return launch_status();
-    }
+    const bool apart = n == 0 || n > GRAD_SUMS;
+    if (apart) grad_norm_kernel<<<1, 256, 0, st>>>(n, (const double*)ws, norm);
     each_table(grads, count, GRAD_CLIP_WGS, [&](const GradTable& t, int wgs) {
-        grad_scale_kernel<<<wgs, 256, 0, st>>>(t, max_norm, n, (const double*)ws, norm);
+        grad_scale_kernel<<<wgs, 256, 0, st>>>(t, max_norm, apart ? 0 : n, (const double*)ws, norm);
     });
     return launch_status();
 }

@@ -105,6 +105,10 @@ def test_a_norm_that_is_not_finite_leaves_the_gradients(bad):
         assert torch.equal(torch.nan_to_num(o), torch.nan_to_num(s)) and torch.equal(torch.isnan(o), torch.isnan(s))
 
 
+def test_tensors_of_several_launches():
+    check(make([16384 + i for i in range(330)], 4), 0.3, True)      # more sums than a clipping launch adds up itself
+
+
 def test_same_result_every_time_and_captured():
     t = make((3_000_001, 70_001, 55), 6)
     outs = [torch.empty_like(x) for x in t]
