@@ -412,8 +412,8 @@ typedef struct {
  * Ties go to the smaller id, of groups and of experts.  The bias decides who is chosen and has
  * no part in the weights.  An expert whose logit is -inf (masked) scores 0 and is chosen only
  * where its token has no other; a NaN logit counts as -inf in the choice.  A logistic score below
- * 1e-299 (a logit below -690) counts as 0.  The weights of a token whose chosen scores are all 0 are 0.  Infinite logits and NaN give undefined weights, never an
- * index out of range.  Tokens with token_mask[t] == 0 (padding) get choices -1 and weights 0, and
+ * 1e-299 (a logit below -690) counts as 0.  The weights of a token whose chosen scores are all
+ * 0 are 0.  Infinite logits and NaN give undefined weights, never an index out of range.  Tokens with token_mask[t] == 0 (padding) get choices -1 and weights 0, and
  * their logits are not read. */
 int moe_router_fwd(const moe_router* router, const float* logits, const float* select_bias_or_null,
                    const uint8_t* token_mask_or_null, int32_t* expert_idx, float* gate_w, void* stream);
@@ -453,13 +453,13 @@ int moe_router_bias_update(const moe_router* router, const int32_t* expert_start
  *   weights  q[E, Np, Kp] and b[E, Np/128, Kb], the matrices [K, N] transposed, Np = N rounded up
  *            to 128: a block is 128 x 128
  * Entries behind K and N are 0, bytes behind Kp / 128 are 127.  A value that is not finite becomes
- * NaN, and the finite values of its block are rounded with an exponent of 120 or more.  All
- * arrays start on 16 bytes.
+ * NaN, and the finite values of its block are rounded with an exponent of 120 or more.
+ * Values, 8-bit or not, start on 16 bytes, exponent bytes on 4 (else MOE_ERR_SHAPE).
  * Rows are grouped by expert as moe_sort_choices does it: expert e has the rows expert_start[e]
  * .. expert_start[e+1]-1; entries of expert_start outside 0..rows count as the nearest of the two,
  * and they must not decrease.  Rows behind the last expert's are neither read nor written.
- * Limits: K, N, d_model, d_ff multiples of 8 from 8 to 2^20; 1 <= E <= 256; rows and T*k < 2^30; one expert's weights
- * Np * Kp < 2^31 (else MOE_ERR_SHAPE). */
+ * Limits: K, N, d_model, d_ff multiples of 8 from 8 to 2^20; 1 <= E <= 256; rows and T*k < 2^30;
+ * one expert's weights Np * Kp < 2^31 (else MOE_ERR_SHAPE). */
 int moe_quantise_rows_fp8(int32_t rows, int32_t K, int32_t dtype, const void* x, void* q, uint8_t* b,
                           void* stream);
 /* W[E,K,N] of type dtype */

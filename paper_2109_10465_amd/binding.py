@@ -489,7 +489,8 @@ def moe_layer_fwd_fp8(shape, router, logits_given, buffers, x, Wg, select_bias, 
 
 
 def moe_fp8_kernels(shape):
-    """(first, second): 0 = tiles of 256 x 256, 1 = of 128 x 128, 2 = of 32 x 32 with a split reduction."""
+    """(first, second): 0 = tiles of 256 x 256, 1 = of 128 x 128, 2 = of 32 x 32 with a split reduction, 3 = of 128
+    columns x 64 rows."""
     first, second = ctypes.c_int32(), ctypes.c_int32()
     _check(lib().moe_fp8_kernels(ctypes.byref(shape), ctypes.byref(first), ctypes.byref(second)), "moe_fp8_kernels")
     return first.value, second.value
@@ -498,7 +499,7 @@ def moe_fp8_kernels(shape):
 # ---- gradients of many tensors -------------------------------------------------------
 class Grads:
     """The list that moe_grad_norm and moe_clip_grads take: pairs (grad, out) of contiguous tensors of one type and
-    length; out may be grad itself, or None for the norm alone.  Keeps its tensors alive."""
+    length; out may be grad itself, or None for the norm alone, and is no other pair's.  Keeps its tensors alive."""
 
     def __init__(self, pairs):
         self.pairs = [tuple(p) for p in pairs]
@@ -510,6 +511,9 @@ class Grads:
                 if t.dtype != g.dtype or t.numel() != g.numel():
                     raise MoeError("a gradient and its output must agree in type and length")
             m.grad, m.out, m.n, m.dtype = _p(g), _p(o), g.numel(), _dtype_of(g)
+        outs = [_p(o) for _, o in self.pairs if o is not None and o.numel()]
+        if len(set(outs)) != len(outs):
+            raise MoeError("an output is in the list twice")
 
 
 def make_grads(pairs):

@@ -82,13 +82,15 @@ extern "C" int moe_quantise_rows_fp8(int32_t rows, int32_t K, int32_t dtype, con
     int rc = begin_call(fp8_extent_status(rows, 1, K, 128, dtype));
     if (rc) return rc;
     if (!x || !q || !b) return MOE_ERR_NULL;
+    if (!aligned(16, x, q) || !aligned(4, b)) return MOE_ERR_SHAPE;
     launch_rows<false>(rows, K, dtype, 1, rows, x, nullptr, q, b, (hipStream_t)stream);
     return launch_status();
 }
 
 int dispatch_fp8_check(const moe_fp8_shape* s, const void* x, const int32_t* row_of, const void* xq, const uint8_t* xb) {
     const int rc = fp8_shape_status(s);
-    return rc ? rc : x && row_of && xq && xb ? MOE_OK : MOE_ERR_NULL;
+    if (rc) return rc;
+    return !(x && row_of && xq && xb) ? MOE_ERR_NULL : aligned(16, x, xq) && aligned(4, xb) ? MOE_OK : MOE_ERR_SHAPE;
 }
 
 extern "C" int moe_dispatch_fp8(const moe_fp8_shape* shape, const void* x, const int32_t* row_of, void* xq, uint8_t* xb,
@@ -162,6 +164,7 @@ extern "C" int moe_quantise_weights_fp8(int32_t E, int32_t K, int32_t N, int32_t
     int rc = begin_call(fp8_extent_status(1, E, K, N, dtype));
     if (rc) return rc;
     if (!W || !q || !b) return MOE_ERR_NULL;
+    if (!aligned(16, W, q) || !aligned(4, b)) return MOE_ERR_SHAPE;
     const int nkb = fp8_blocks(K), nnb = fp8_blocks(N);
     const dim3 grid(nkb, nnb, E);
     hipStream_t st = (hipStream_t)stream;

@@ -559,6 +559,7 @@ extern "C" int moe_expert_product_fp8(int32_t rows, int32_t E, int32_t K, int32_
     int rc = begin_call(fp8_extent_status(rows, E, K, N, y_dtype));
     if (rc) return rc;
     if (!xq || !xb || !expert_start || !Wq || !Wb || !y) return MOE_ERR_NULL;
+    if (!aligned(16, xq, Wq, y) || !aligned(4, xb, Wb)) return MOE_ERR_SHAPE;
     const Fp8Args p = fp8_args(rows, E, K, N, xq, xb, expert_start, Wq, Wb, y, nullptr);
     rc = y_dtype == MOE_BF16 ? launch_fp8<OUT_BF16>(p, (hipStream_t)stream) : launch_fp8<OUT_F32>(p, (hipStream_t)stream);
     return rc ? rc : launch_status();
@@ -577,7 +578,8 @@ int ffn_fp8_check(const moe_fp8_shape* s, const void* xq, const uint8_t* xb, con
     const int rc = fp8_shape_status(s);
     if (rc) return rc;
     if (yd_dtype != MOE_F32 && yd_dtype != MOE_BF16) return MOE_ERR_DTYPE;
-    return xq && xb && expert_start && W1q && W1b && W2q && W2b && hq && hb && yd ? MOE_OK : MOE_ERR_NULL;
+    if (!(xq && xb && expert_start && W1q && W1b && W2q && W2b && hq && hb && yd)) return MOE_ERR_NULL;
+    return aligned(16, xq, W1q, W2q, hq, yd) && aligned(4, xb, W1b, W2b, hb) ? MOE_OK : MOE_ERR_SHAPE;
 }
 
 extern "C" int moe_expert_ffn_fwd_fp8(const moe_fp8_shape* shape, const void* xq, const uint8_t* xb,

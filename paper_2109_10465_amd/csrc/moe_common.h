@@ -300,6 +300,7 @@ static inline int begin_call(int check) {
     return check;
 }
 static inline int check_shape(const moe_shape* s) { return begin_call(shape_status(s)); }
+template <typename... P> static inline bool aligned(int bytes, P... p) { return (((uintptr_t)p | ...) & (bytes - 1)) == 0; }
 static inline bool ws_ok(const void* ws, size_t ws_bytes, size_t need) {
     return ws && !((uintptr_t)ws & 255) && ws_bytes >= need;
 }

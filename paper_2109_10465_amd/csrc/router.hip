@@ -5,6 +5,7 @@
 #include "moe_common.h"
 
 #define ROUTER_MAX_K 8
+#define ROUTER_TOKENS (1 << 25)  // of a launch: 64 threads for each, and a grid has fewer than 2^32
 #define LOGISTIC_ZERO -690.0f    // logits below have a logistic score under 1e-299, which counts as 0 (as exp overflows it does in 64 bits)
 
 // ---------------------------------------------------------------------------
@@ -24,7 +25,7 @@ struct RouterArgs {
     int T, E, k, score, n_groups, group, top_groups, group_best, renormalise;   // group = experts per group
     float scale;
     int lg_log2;                    // lanes per group
-    int vec;                        // a lane's experts start on 16 bytes and are eight
+    int vec;                        // a lane's experts start on 16 bytes and are eight (backward: are four)
 };
 
 __device__ __forceinline__ double score64(double l, bool sigmoid, double top, double total) {
@@ -291,7 +292,7 @@ __global__ __launch_bounds__(256) void router_bwd_kernel(const RouterArgs a, con
         dw = dgate_w[(size_t)t * a.k + sub];
     }
     float out[4] = {0.0f, 0.0f, 0.0f, 0.0f}, l[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    const bool vec = (a.E & 3) == 0, dense = !sigmoid && !a.renormalise;    // (the renormalised softmax's q sum to 0)
+    const bool dense = !sigmoid && !a.renormalise;    // (the renormalised softmax's q sum to 0)
     const bool none = x == -INFINITY || (sigmoid && x < LOGISTIC_ZERO);
     float r = 0.0f, top = 0.0f, inv = 1.0f, mean = 0.0f;
     if (dense) {
@@ -332,7 +333,7 @@ __global__ __launch_bounds__(256) void router_bwd_kernel(const RouterArgs a, con
     }
     if (!in) return;
     float* o = dlogits + (size_t)t * a.E;
-    if (vec) {
+    if (a.vec) {
         if (e4 < a.E) *reinterpret_cast<float4*>(o + e4) = make_float4(out[0], out[1], out[2], out[3]);
     } else {
 #pragma unroll
@@ -380,10 +381,17 @@ extern "C" int moe_router_fwd(const moe_router* router, const float* logits, con
     a.vec = a.group % 8 == 0 && (((uintptr_t)logits | (uintptr_t)select_bias_or_null) & 15) == 0;
     const int lanes = a.lg_log2 + log2_up(r.n_groups);
     hipStream_t st = (hipStream_t)stream;
-#define FWD(LPT) (select_bias_or_null ? router_fwd_kernel<LPT, true> : router_fwd_kernel<LPT, false>)<<<ceil_div(r.T, 256 / LPT), 256, 0, st>>>( \
-    a, logits, select_bias_or_null, token_mask_or_null, expert_idx, gate_w)
-    if (lanes <= 3) FWD(8); else if (lanes == 4) FWD(16); else if (lanes == 5) FWD(32); else FWD(64);
+    for (int t = 0; t < r.T; t += ROUTER_TOKENS) {
+        a.T = r.T - t < ROUTER_TOKENS ? r.T - t : ROUTER_TOKENS;
+        const float* l = logits + (size_t)t * r.E;
+        const uint8_t* m = token_mask_or_null ? token_mask_or_null + t : nullptr;
+        int32_t* id = expert_idx + (size_t)t * r.k;
+        float* w = gate_w + (size_t)t * r.k;
+#define FWD(LPT) (select_bias_or_null ? router_fwd_kernel<LPT, true> : router_fwd_kernel<LPT, false>)<<<ceil_div(a.T, 256 / LPT), 256, 0, st>>>( \
+    a, l, select_bias_or_null, m, id, w)
+        if (lanes <= 3) FWD(8); else if (lanes == 4) FWD(16); else if (lanes == 5) FWD(32); else FWD(64);
 #undef FWD
+    }
     return launch_status();
 }
 
@@ -393,13 +401,18 @@ extern "C" int moe_router_bwd(const moe_router* router, const float* logits, con
     if (rc) return rc;
     if (!logits || !expert_idx || !dgate_w || !dlogits) return MOE_ERR_NULL;
     const moe_router& r = *router;
-    const RouterArgs a = {r.T, r.E, r.k, r.score, r.n_groups, r.E / r.n_groups, r.top_groups, r.group_best, r.renormalise != 0,
-                          r.scale, 0, 0};
+    RouterArgs a = {r.T, r.E, r.k, r.score, r.n_groups, r.E / r.n_groups, r.top_groups, r.group_best, r.renormalise != 0,
+                    r.scale, 0, 0};
+    a.vec = r.E % 4 == 0 && ((uintptr_t)dlogits & 15) == 0;
     const int lanes = log2_up(ceil_div(r.E, 4));
     hipStream_t st = (hipStream_t)stream;
-#define BWD(LPT) router_bwd_kernel<LPT><<<ceil_div(r.T, 256 / LPT), 256, 0, st>>>(a, logits, expert_idx, dgate_w, dlogits)
-    if (lanes <= 3) BWD(8); else if (lanes == 4) BWD(16); else if (lanes == 5) BWD(32); else BWD(64);
+    for (int t = 0; t < r.T; t += ROUTER_TOKENS) {
+        a.T = r.T - t < ROUTER_TOKENS ? r.T - t : ROUTER_TOKENS;
+        const size_t l = (size_t)t * r.E, c = (size_t)t * r.k;
+#define BWD(LPT) router_bwd_kernel<LPT><<<ceil_div(a.T, 256 / LPT), 256, 0, st>>>(a, logits + l, expert_idx + c, dgate_w + c, dlogits + l)
+        if (lanes <= 3) BWD(8); else if (lanes == 4) BWD(16); else if (lanes == 5) BWD(32); else BWD(64);
 #undef BWD
+    }
     return launch_status();
 }
 
@@ -646,29 +659,30 @@ template <typename T>
 __global__ __launch_bounds__(256) void combine_rows_kernel(int Tn, int d, int k, int R, const T* __restrict__ yd,
                                                            const int32_t* __restrict__ row_of,
                                                            const float* __restrict__ gate_w, bf16_t* __restrict__ y) {
-    const int lane = threadIdx.x & 63, t = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (t >= Tn) return;
-    int row[ROUTER_MAX_K];
-    float w[ROUTER_MAX_K];
-#pragma unroll
-    for (int j = 0; j < ROUTER_MAX_K; ++j) {
-        const int r = j < k ? row_of[(size_t)t * k + j] : -1;
-        row[j] = (unsigned)r < (unsigned)R ? r : -1;
-        w[j] = row[j] >= 0 ? gate_w[(size_t)t * k + j] : 0.0f;
-    }
-    for (int v = lane; v < d / 8; v += 64) {
-        float acc[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
+    const int lane = threadIdx.x & 63;
+    for (int t = blockIdx.x * 4 + (threadIdx.x >> 6); t < Tn; t += gridDim.x * 4) {
+        int row[ROUTER_MAX_K];
+        float w[ROUTER_MAX_K];
 #pragma unroll
         for (int j = 0; j < ROUTER_MAX_K; ++j) {
-            if (row[j] < 0) continue;
-            float b[8];
-            row8(yd + (size_t)row[j] * d + (size_t)v * 8, b);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], b[i], acc[i]);
+            const int r = j < k ? row_of[(size_t)t * k + j] : -1;
+            row[j] = (unsigned)r < (unsigned)R ? r : -1;
+            w[j] = row[j] >= 0 ? gate_w[(size_t)t * k + j] : 0.0f;
         }
-        Chunk<bf16_t>::store(y + (size_t)t * d + (size_t)v * 8, acc);
+        for (int v = lane; v < d / 8; v += 64) {
+            float acc[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < ROUTER_MAX_K; ++j) {
+                if (row[j] < 0) continue;
+                float b[8];
+                row8(yd + (size_t)row[j] * d + (size_t)v * 8, b);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] = fmaf(w[j], b[i], acc[i]);
+            }
+            Chunk<bf16_t>::store(y + (size_t)t * d + (size_t)v * 8, acc);
+        }
     }
 }
 
@@ -677,14 +691,14 @@ int combine_rows_check(const moe_fp8_shape* s, int yd_dtype, const void* yd, con
     const int rc = fp8_shape_status(s);
     if (rc) return rc;
     if (yd_dtype != MOE_F32 && yd_dtype != MOE_BF16) return MOE_ERR_DTYPE;
-    return yd && row_of && gate_w && y ? MOE_OK : MOE_ERR_NULL;
+    return !(yd && row_of && gate_w && y) ? MOE_ERR_NULL : aligned(16, yd, y) ? MOE_OK : MOE_ERR_SHAPE;
 }
 
 extern "C" int moe_combine_rows(const moe_fp8_shape* shape, int32_t yd_dtype, const void* yd, const int32_t* row_of,
                                 const float* gate_w, void* y, void* stream) {
     const int rc = begin_call(combine_rows_check(shape, yd_dtype, yd, row_of, gate_w, y));
     if (rc) return rc;
-    const int grid = ceil_div(shape->T, 4), R = shape->T * shape->k;
+    const int tokens = ceil_div(shape->T, 4), grid = tokens < ROUTER_TOKENS / 4 ? tokens : ROUTER_TOKENS / 4, R = shape->T * shape->k;
     hipStream_t st = (hipStream_t)stream;
     if (yd_dtype == MOE_BF16)
         combine_rows_kernel<bf16_t><<<grid, 256, 0, st>>>(shape->T, shape->d_model, shape->k, R, (const bf16_t*)yd, row_of, gate_w, (bf16_t*)y);

@@ -125,13 +125,17 @@ class MoELayer:
         or bfloat16, contiguous) to the global norm max_norm, in place, and returns that norm (a device tensor of one float)."""
         if self.forward_only:
             raise B.MoeError("this layer was built forward-only")
+        for g in others:
+            if g.device != self.dWg.device:
+                raise B.MoeError(f"a gradient on {g.device}, not {self.dWg.device}")
         grads = B.make_grads([(g, g) for g in (self.dWg, self.dW1, self.dW2, *others)])
         need = B.moe_grad_workspace_bytes(grads)
         if self._clip is None or self._clip[1].numel() < need:
             self._clip = (torch.empty(1, dtype=torch.float32, device=self.device),
                           torch.empty(need, dtype=torch.uint8, device=self.device))
         norm, ws = self._clip
-        B.moe_clip_grads(grads, max_norm, norm, ws)
+        with torch.cuda.device(self.device):
+            B.moe_clip_grads(grads, max_norm, norm, ws)
         return norm
 
     _clip = None        # norm and workspace of clip_gradients
@@ -164,6 +168,7 @@ class Fp8MoELayer:
                 raise B.MoeError("8-bit weights must be contiguous")
         self.W1, self.W2 = W1, W2
         self.device = torch.device(device)
+        B.moe_fp8_kernels(self.shape)           # (refuses what the experts' block refuses)
         R = T * k
 
         def buf(shape, dt):
@@ -177,28 +182,49 @@ class Fp8MoELayer:
         self.hq, self.hb = buf((R, B.fp8_padded(d_ff)), u8), buf((R, B.fp8_scale_bytes(d_ff)), u8)
         self.yd, self.y = buf((R, d_model), torch.float32), buf((T, d_model), _TORCH_DT[dtype])
         self.ws = buf((nbytes,), u8)
+        for t in (*W1, *W2):
+            if t.device != self.y.device:
+                raise B.MoeError(f"8-bit weights on {t.device}, not {self.y.device}")
+        # what forward() takes: shape and type
+        f32 = torch.float32
+        self._takes = {"x": ((T, d_model), self.y.dtype), "Wg": ((d_model, E), f32), "logits": ((T, E), f32),
+                       "select_bias": ((E,), f32), "token_mask": ((T,), u8)}
+
+    def _check(self, name, t):
+        shape, dt = self._takes[name]
+        if t is not None and (tuple(t.shape) != shape or t.dtype != dt or t.device != self.y.device or not t.is_contiguous()):
+            raise B.MoeError(f"{name}: contiguous {dt} of {shape} on {self.y.device} expected, not {t.dtype} of {tuple(t.shape)} "
+                             f"with strides {t.stride()} on {t.device}")
 
     @staticmethod
     def quantise_weights(W):
         """W [E, K, N] (float32 or bfloat16, on the GPU) -> (q, b) as the experts take them."""
         E, K, N = W.shape
-        if not W.is_contiguous():
-            raise B.MoeError("weights must be contiguous")
+        if not (W.is_contiguous() and W.is_cuda):
+            raise B.MoeError("weights must be contiguous and on a GPU")
         q = torch.empty((E, B.fp8_padded(N), B.fp8_padded(K)), dtype=torch.float8_e4m3fn, device=W.device)
         b = torch.empty((E, B.fp8_padded(N) // 128, B.fp8_scale_bytes(K)), dtype=torch.uint8, device=W.device)
-        B.moe_quantise_weights_fp8(E, K, N, W, q, b)
+        with torch.cuda.device(W.device):
+            B.moe_quantise_weights_fp8(E, K, N, W, q, b)
         return q, b
 
     def forward(self, x, Wg=None, logits=None, select_bias=None, token_mask=None):
         """x [T, d_model]; Wg [d_model, E] fp32, or logits [T, E] fp32 in its place; select_bias [E] fp32; token_mask [T]
-        uint8, 0 for padding (its rows of y are 0)."""
+        uint8 or bool, 0 for padding (its rows of y are 0)."""
         if (Wg is None) == (logits is None):
             raise B.MoeError("either Wg or logits")
+        if token_mask is not None and token_mask.dtype == torch.bool:
+            token_mask = token_mask.view(torch.uint8)
+        for name, t in (("x", x), ("Wg", Wg), ("logits", logits), ("select_bias", select_bias), ("token_mask", token_mask)):
+            self._check(name, t)
         ptrs = [(logits if n == "logits" and logits is not None else getattr(self, n)).data_ptr() for n in self._NAMES]
-        B.moe_layer_fwd_fp8(self.shape, self.router, logits is not None, B.Fp8Buffers(*ptrs, self.ws.numel()), x, Wg,
-                            select_bias, token_mask, *self.W1, *self.W2)
+        with torch.cuda.device(self.device):
+            B.moe_layer_fwd_fp8(self.shape, self.router, logits is not None, B.Fp8Buffers(*ptrs, self.ws.numel()), x, Wg,
+                                select_bias, token_mask, *self.W1, *self.W2)
         return self.y
 
     def update_select_bias(self, select_bias, rate):
         """After a forward pass: raises the bias of experts with fewer choices than the mean by rate, lowers the others'."""
-        B.moe_router_bias_update(self.router, self.expert_start, rate, select_bias)
+        self._check("select_bias", select_bias)
+        with torch.cuda.device(self.device):
+            B.moe_router_bias_update(self.router, self.expert_start, rate, select_bias)

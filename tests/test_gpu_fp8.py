@@ -369,5 +369,28 @@ def test_layer_refuses_weights_of_another_layout():
         Fp8MoELayer(8, 128, 256, 4, 2, B.BF16, B.GELU, (q, b), (q, b))
     q2, b2 = Fp8MoELayer.quantise_weights(torch.randn(4, 256, 128).cuda())
     layer = Fp8MoELayer(8, 128, 256, 4, 2, B.BF16, B.GELU, (q, b), (q2, b2))
+    x = torch.zeros(8, 128, dtype=torch.bfloat16, device="cuda")
     with pytest.raises(B.MoeError):
-        layer.forward(torch.zeros(8, 128, dtype=torch.bfloat16, device="cuda"))
+        layer.forward(x)
+    l, bias, mask = torch.zeros(8, 4, device="cuda"), torch.zeros(4, device="cuda"), torch.ones(8, dtype=torch.uint8, device="cuda")
+    layer.forward(x, logits=l, select_bias=bias, token_mask=mask.bool())
+    for bad in (dict(x=x[:7]), dict(x=x.float()), dict(x=x.cpu()), dict(x=x.t().contiguous().t()), dict(logits=l.double()),
+                dict(logits=l[:, :3]), dict(select_bias=bias[:3]), dict(token_mask=mask.int())):
+        with pytest.raises(B.MoeError):
+            layer.forward(**{**dict(x=x, logits=l, select_bias=bias, token_mask=mask), **bad})
+    with pytest.raises(B.MoeError):
+        Fp8MoELayer(8, 128, 256, 4, 2, B.BF16, B.GELU, (q.cpu(), b), (q2, b2))
+    with pytest.raises(B.MoeError):
+        Fp8MoELayer.quantise_weights(torch.randn(4, 256, 128))
+
+
+def test_mixture_of_more_tokens_than_a_grid_has():
+    T = (1 << 25) + 5
+    s = B.make_fp8_shape(T, 8, 8, 4, 1, B.BF16, B.RELU)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    yd, w = torch.randn((T, 8), generator=g, device="cuda"), torch.rand((T, 1), generator=g, device="cuda")
+    row_of = torch.arange(T - 1, -1, -1, dtype=torch.int32, device="cuda")
+    y = torch.empty((T, 8), dtype=torch.bfloat16, device="cuda")
+    B.moe_combine_rows(s, yd, row_of, w, y)
+    torch.cuda.synchronize()
+    assert torch.equal(y, (yd.flip(0) * w).bfloat16())      # one product, one rounding of it

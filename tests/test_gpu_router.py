@@ -195,6 +195,29 @@ def test_bias_update():
         assert torch.equal(bias.cpu(), want)
 
 
+def test_more_tokens_than_a_launch_has():
+    T = (1 << 25) + 5
+    r = B.make_router(T, 8, 1, B.SOFTMAX, renormalise=False)
+    l = torch.randn((T, 8), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    mask = torch.ones(T, dtype=torch.uint8, device="cuda")
+    mask[T - 2] = mask[7] = 0
+    idx, w = torch.empty((T, 1), dtype=torch.int32, device="cuda"), torch.empty((T, 1), device="cuda")
+    B.moe_router_fwd(r, l, None, mask, idx, w)
+    dw, dl = torch.ones((T, 1), device="cuda"), torch.empty_like(l)
+    B.moe_router_bwd(r, l, idx, dw, dl)
+    torch.cuda.synchronize()
+    on = mask != 0
+    assert (idx[~on] == -1).all() and (w[~on] == 0).all() and (dl[~on] == 0).all()
+    assert torch.equal(l.gather(1, idx.long().clamp(min=0))[on, 0], l.amax(1)[on])
+    for at in (slice(0, 7), slice((1 << 25) - 4, (1 << 25) + 3)):
+        s = torch.softmax(l[at].double(), 1)
+        best, e = s.max(1, keepdim=True)
+        want = -best * s
+        want.scatter_add_(1, e, best)
+        # (scores of at most 1 from exponentials within 2^-20)
+        assert (w[at].double() - best).abs().max() <= 2.0 ** -18 and (dl[at].double() - want).abs().max() <= 2.0 ** -18
+
+
 def test_captured_and_replayed_on_another_stream():
     r = B.make_router(300, 96, 4, B.SIGMOID, 8, 3, 2, True, 2.0)
     l, b, m = inputs(r, 8, True, pad=0.1)

@@ -112,6 +112,23 @@ def test_fp8_extents(rows, E, K, N, dtype, code):
         assert L.moe_quantise_rows_fp8(rows, K, dtype, P, P, P, None) == code
 
 
+def test_fp8_alignment():
+    L, s = B.lib(), shape()
+    ffn = lambda s, *a: L.moe_expert_ffn_fwd_fp8(s, *a[:9], 0, *a[9:])
+    combine = lambda s, *a: L.moe_combine_rows(s, 1, *a)
+    product = lambda *a: L.moe_expert_product_fp8(4, 2, 128, 64, *a[:5], 1, *a[5:])
+    rows, weights = (lambda *a: L.moe_quantise_rows_fp8(4, 128, 0, *a)), (lambda *a: L.moe_quantise_weights_fp8(2, 128, 64, 0, *a))
+    # per entry: the arguments that are values, and those that are exponents
+    for f, n, values, exponents in ((lambda *a: L.moe_dispatch_fp8(REF(s), *a), 4, (0, 2), (3,)),
+                                    (lambda *a: ffn(REF(s), *a), 10, (0, 3, 5, 7, 9), (1, 4, 6, 8)),
+                                    (lambda *a: combine(REF(s), *a), 4, (0, 3), ()), (product, 6, (0, 3, 5), (1, 4)),
+                                    (rows, 3, (0, 1), (2,)), (weights, 3, (0, 1), (2,))):
+        for i in (*values, *exponents):
+            a = [P] * n
+            a[i] = P + (8 if i in values else 2)
+            assert f(*a, None) == -2, (n, i)
+
+
 def test_fp8_layer_reports_every_error_before_its_first_launch():
     L, r, s = B.lib(), router(), shape()
 
@@ -166,6 +183,8 @@ def test_grads_of_tensors():
     for pair in ((a.t()[:2], None), (a, b), (a, torch.zeros(15)), (a.half(), None)):
         with pytest.raises(B.MoeError):
             B.make_grads([pair])
+    with pytest.raises(B.MoeError):                 # clipped twice
+        B.make_grads([(a, a), (b, b), (a, a)])
 
 
 def test_extents_of_the_8_bit_format():
