@@ -238,11 +238,16 @@ __global__ __launch_bounds__(256) void router_fwd_kernel(const RouterArgs a, con
         }
     }
     float mine = 0.0f, behind = 0.0f;       // lane j: the j-th choice and the one after it
+    // Two lanes can have the same key, which would then both move on, and one choice be lost: a round has one owner per token.
+    const unsigned long long live = __ballot(valid);
+    const int tokens = __popcll(live) / LPT;
+    bool shared = false;
     for (int j = 0; j <= a.k; ++j) {        // one more than are chosen
         const float w = token_max<LPT>(key[0]);
         mine = sub == j ? w : mine;
         behind = sub + 1 == j ? w : behind;
         if (j == a.k) break;
+        shared |= __popcll(__ballot(key[0] == w) & live) != tokens;
         if (key[0] == w) {
             s_choice[j] = e0 + (int)(__float_as_uint(w) & 7u);
 #pragma unroll
@@ -251,7 +256,7 @@ __global__ __launch_bounds__(256) void router_fwd_kernel(const RouterArgs a, con
         }
     }
     again |= sub < a.k && near(mine, behind);
-    if (__any(valid && again)) choose64<LPT, BIAS>(a, row, bias, valid, here, e0, g, sub, s_choice);
+    if (shared || __any(valid && again)) choose64<LPT, BIAS>(a, row, bias, valid, here, e0, g, sub, s_choice);
     __builtin_amdgcn_wave_barrier();
     // the token's choices and weights: lane j has the j-th
     const int id = sub < a.k && valid ? s_choice[sub] : -1;

@@ -119,6 +119,26 @@ def test_near_ties_are_decided_in_64_bits():
         assert torch.equal(idx.cpu(), ref)
 
 
+@pytest.mark.parametrize("E,k,score", [(16, 1, B.SOFTMAX), (24, 3, B.SIGMOID), (64, 8, B.SOFTMAX), (136, 2, B.SIGMOID), (256, 8, B.SIGMOID)])
+def test_near_ties_of_equal_places(E, k, score):
+    """The same entry of two lanes' eights, a step of fp32 apart or equal: once at every rank, the last and the one behind it too."""
+    T, rng = 512, np.random.default_rng(E)
+    l = rng.standard_normal((T, E)).astype(np.float32)
+    for t in range(T):
+        rank = t % (k + 1)
+        e = int(np.argsort(-l[t])[rank])
+        o = (e + 8 * int(rng.integers(1, E // 8))) % (E // 8 * 8)
+        l[t, o] = (l[t, e], np.nextafter(l[t, e], np.float32(9)), np.nextafter(l[t, e], np.float32(-9)))[t // (k + 1) % 3]
+    l = torch.from_numpy(l)
+    b = torch.zeros(E)
+    mask = torch.from_numpy((rng.random(T) < 0.9).astype(np.uint8))
+    for bias in (None, b):
+        for m in (None, mask):
+            r = B.make_router(T, E, k, score)
+            got, ref = forward(r, l, bias, m)[0].cpu(), R.route(r, l, bias, m)[0]
+            assert torch.equal(got, ref), (got != ref).any(1).nonzero()[:5].tolist()
+
+
 def test_gradient_against_differences():
     r = B.make_router(16, 24, 3, B.SIGMOID, 4, 2, 2, True, 1.5)
     l, b, _ = inputs(r, 11, True)
