@@ -212,7 +212,7 @@ __global__ __launch_bounds__(256) void router_fwd_kernel(const RouterArgs a, con
     order(1, 4); order(3, 6);
     order(2, 4); order(3, 5);
     order(3, 4);
-    // How far apart two values have to be: a key drops three bits (2^-20 of its size), a score is off by less than 5e-7
+    // How far apart two choices have to be: a key drops three bits (2^-20 of its size), a score is off by less than 5e-7
     // (exponential, reciprocal and their argument), the sum with the bias by 2^-24: twice that, and a half more.
     auto near = [](float hi, float lo) { return hi - lo <= fmaf(fabsf(hi) + fabsf(lo), 1.6e-6f, 1.6e-6f); };
     bool again = false;
@@ -226,11 +226,16 @@ __global__ __launch_bounds__(256) void router_fwd_kernel(const RouterArgs a, con
         float gv = b0;
         if (a.group_best == 2) gv = b1 < -2.95e38f ? KEY_DEAD : BIAS ? b0 + b1 : score(b0) + score(b1);
         if (g >= a.n_groups) gv = KEY_OUT;
+        // A group's value is off by its keys' and scores' errors; where a score is made of a key, by that score's share of the
+        // logit's (a softmax does not mind how large logits are, a key does).  The token's largest such error, twice, is near.
+        float off = fmaf(fabsf(b0) + (a.group_best == 2 ? fabsf(b1) : 0.0f), 1.6e-6f, 1.6e-6f);
+        if (!BIAS && a.group_best == 2) off = fmaf(fabsf(b0) + fabsf(b1), gv * 1.6e-6f, 1.6e-6f);
+        off = 2.0f * token_max<LPT>(gv < -2.95e38f ? 0.0f : off);
         int before = 0;
         for (int o = 1; o < LPT >> a.lg_log2; ++o) {
             const float w = __shfl_xor(gv, o << a.lg_log2, MOE_WAVE);
             before += w > gv;
-            again |= (g ^ o) < a.n_groups && g < a.n_groups && near(fmaxf(w, gv), fminf(w, gv));
+            again |= (g ^ o) < a.n_groups && g < a.n_groups && fabsf(w - gv) <= off;
         }
         if (before >= a.top_groups) {
 #pragma unroll

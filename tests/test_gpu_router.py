@@ -139,6 +139,42 @@ def test_near_ties_of_equal_places(E, k, score):
             assert torch.equal(got, ref), (got != ref).any(1).nonzero()[:5].tolist()
 
 
+@pytest.mark.parametrize("how", ["shifted", "cancelled"])
+def test_groups_that_differ_by_little(how):
+    """Sums of a group's best two that differ by less than keys of 32 bits can tell: logits far from 0 whose softmax does not
+    mind, and biases that take the scores away."""
+    T, E, G = 512, 64, 4
+    rng = np.random.default_rng(11)
+    l = rng.standard_normal((T, E)).astype(np.float32)
+    l[:, ::16] += np.float32(4.0)               # a group's best
+    b = None
+    if how == "shifted":
+        l += np.float32(200.0)
+        for t in range(T):                      # groups that are another one's copy but for a few steps of fp32
+            l[t, 48:] = np.roll(l[t, 32:48], 5)
+            l[t, 16:32] = np.roll(l[t, :16], 3)
+            for e in (19, 53):
+                for _ in range(1 + t % 5):
+                    l[t, e] = np.nextafter(l[t, e], np.float32(300 if t % 2 else 0))
+    else:
+        b = np.zeros(E, dtype=np.float32)
+        b[::16] = 5.0
+        b[1::16] = np.float32([-5.9, -5.90001, -5.900004, -5.9])
+        b[2:16] = b[18:32] = b[34:48] = b[50:] = -20.0
+        l[:, 1:16] = l[:, 1:2]
+        for q in range(1, 4):
+            l[:, 16 * q:16 * q + 16] = l[:, :16]
+        l[:, 16] += (rng.standard_normal(T) * 1e-4).astype(np.float32)
+        for q in range(4):
+            l[:, 16 * q:16 * q + 16] = np.roll(l[:, 16 * q:16 * q + 16], 2 * q + 1, 1)
+            b[16 * q:16 * q + 16] = np.roll(b[16 * q:16 * q + 16], 2 * q + 1)
+    l, b = torch.from_numpy(l), None if b is None else torch.from_numpy(b)
+    for top in (1, 3):
+        r = B.make_router(T, E, 2, B.SOFTMAX if b is None else B.SIGMOID, G, top, 2)
+        got, ref = forward(r, l, b, None)[0].cpu(), R.route(r, l, b, None)[0]
+        assert torch.equal(got, ref), (got != ref).any(1).sum().item()
+
+
 def test_gradient_against_differences():
     r = B.make_router(16, 24, 3, B.SIGMOID, 4, 2, 2, True, 1.5)
     l, b, _ = inputs(r, 11, True)
