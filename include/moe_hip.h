@@ -489,7 +489,9 @@ int moe_dispatch_fp8(const moe_fp8_shape* shape, const void* x, const int32_t* r
 
 /* The experts' block: h = act(x W1) in 8 bits -> hq[R,Kp(d_ff)], hb;  yd[R,d_model] = h W2, of type
  * yd_dtype.  The hidden activation is formed in fp32 and rounded once, to the format
- * above (with exponents not below -126, and NaN passed over in finding them). */
+ * above (with exponents not below -126, and NaN passed over in finding them).  With at most 48 rows per
+ * expert on average its sums are as exact as fp32's: a sum that falls to the other side of a rounding
+ * moves an entry by 6 %, which shows where few rows are all there is. */
 int moe_expert_ffn_fwd_fp8(const moe_fp8_shape* shape, const void* xq, const uint8_t* xb,
                            const int32_t* expert_start, const void* W1q, const uint8_t* W1b,
                            const void* W2q, const uint8_t* W2b, void* hq, uint8_t* hb, int32_t yd_dtype,

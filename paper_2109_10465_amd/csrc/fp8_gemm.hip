@@ -116,6 +116,9 @@ __device__ __forceinline__ void store_byte(const Fp8Args& p, int byte, int nb, i
     else if (nb == p.nnb - 1)
         for (int i = p.nnb; i < p.yb_stride; ++i) bt[i] = 127;
 }
+// a hidden block's exponent byte, of a unit that fp32 holds as a normal number: 2^-126 at least
+__device__ __forceinline__ int block_byte(float top) { return max(1, scale_byte(__float_as_uint(top))); }
+__device__ __forceinline__ float block_unit(int byte) { return __uint_as_float((uint32_t)byte << 23); }
 // all four tiles of a block in one wave
 template <int OUT>
 __device__ __forceinline__ void store_block(const Fp8Args& p, f32x16_t (&acc)[4], int nb, int r, bool live, int half) {
@@ -124,9 +127,8 @@ __device__ __forceinline__ void store_block(const Fp8Args& p, f32x16_t (&acc)[4]
         float top = 0.0f;
 #pragma unroll
         for (int f = 0; f < 4; ++f) top = activate<OUT>(acc[f], top);
-        // (a unit that fp32 holds as a normal number: 2^-126 at least)
-        const int byte = max(1, scale_byte(__float_as_uint(fmaxf(top, __shfl_xor(top, 32, MOE_WAVE)))));
-        unit = __uint_as_float((uint32_t)byte << 23);
+        const int byte = block_byte(fmaxf(top, __shfl_xor(top, 32, MOE_WAVE)));
+        unit = block_unit(byte);
         if (live) store_byte(p, byte, nb, r, half);
     }
 #pragma unroll
@@ -265,6 +267,15 @@ struct Fp8Tile {
 
 struct Fp8Place { int e, row, end, col; };      // a tile: expert, first row, the expert's end, first block of 128 columns
 
+// eight e4m3 values as fp16, which holds them all
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ f16x8_t to_f16(uint32_t lo, uint32_t hi) {
+    const f16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
+    const f16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+    return f16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
 // which tile is number `at` (found by the whole wave)
 template <int BT, int WF>
 __device__ __forceinline__ Fp8Place fp8_place(const int* tiles, const int* start, int at, int ctiles, int lane) {
@@ -285,14 +296,19 @@ __device__ __forceinline__ Fp8Place fp8_place(const int* tiles, const int* start
             __builtin_amdgcn_readfirstlane(col * WF)};
 }
 
-template <int WF, int WT, int TT, int BT, int NS, int OUT>
+// FINE: the products are formed of fp16 operands and added in fp32, slab by slab, so that they are as exact as fp32 sums;
+// the four waves have 32 columns of all rows each, and share the conversion of the columns.  For hidden activations of few
+// rows: they are rounded to 4 bits, where a sum that is 2^-14 off falls to the other side of a tie in 1 of 900 entries, and
+// such steps of 6 % show where few rows are summed (48 rows of 376: outputs 0.3 % off, bf16's rounding 0.17).  The matrix
+// instructions take twice as long, which the weights' bytes hide.
+template <int WF, int WT, int TT, int BT, int NS, int OUT, bool FINE>
 __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args p) {
     typedef Fp8Tile<WF, WT, TT, BT, NS> G;
     extern __shared__ __align__(1024) uint8_t smem[];
     int* tiles = reinterpret_cast<int*>(smem + G::TABLE);
     int* start = tiles + 260;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int l32 = lane & 31, half = lane >> 5, wf = wave % WF, wt = wave / WF;     // (waves without rows are then spread over the SIMDs)
+    const int l32 = lane & 31, half = lane >> 5, wf = wave % WF, wt = FINE ? 0 : wave / WF;     // (waves without rows are then spread over the SIMDs)
     const int ctiles = (p.nnb + WF - 1) / WF;
     if (wave == 0) {
         int s[5], t[4], n = 0;
@@ -404,11 +420,12 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
     for (int s = 0; s < NS - 1; ++s) fetch(s);
     int stage = 0, have = 0;
     for (;;) {
-        f32x16_t acc[TT][4];
+        constexpr int FT = FINE ? 1 : 4;        // matrix tiles side by side
+        f32x16_t acc[TT][FT];
 #pragma unroll
         for (int t = 0; t < TT; ++t)
 #pragma unroll
-            for (int f = 0; f < 4; ++f)
+            for (int f = 0; f < FT; ++f)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[t][f][i] = 0.0f;
         int we = 0, xe[TT] = {};
@@ -429,7 +446,33 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
                 if constexpr (NS > 2) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
             fetch(stage == 0 ? NS - 1 : stage - 1);
-            if (live) {
+            if constexpr (FINE) {
+                const uint8_t* w = smem + stage * G::STAGE + wave * 4096;
+                const uint8_t* x = smem + stage * G::STAGE + G::BF * 128;
+                f16x8_t a[8];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(w + frag[c]);
+                    a[2 * c] = to_f16(v.x, v.y);
+                    a[2 * c + 1] = to_f16(v.z, v.w);
+                }
+#pragma unroll
+                for (int t = 0; t < TT; ++t) {
+                    if (cur.row + 32 * t >= cur.end) break;
+                    f32x16_t part;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) part[i] = 0.0f;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(x + t * 4096 + frag[c]);
+                        part = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[2 * c], to_f16(v.x, v.y), part, 0, 0, 0);
+                        part = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[2 * c + 1], to_f16(v.z, v.w), part, 0, 0, 0);
+                    }
+                    const int e = (we & 255) + (xe[t] & 255) - 254;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[t][0][i] += ldexpf(part[i], e);
+                }
+            } else if (live) {
                 const uint8_t* w = smem + stage * G::STAGE + wbase;
                 const uint8_t* x = smem + stage * G::STAGE + xbase;
 #pragma unroll
@@ -451,7 +494,25 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
             for (int t = 0; t < TT; ++t) xe[t] = (int)((uint32_t)xe[t] >> 8);
             stage = stage == NS - 1 ? 0 : stage + 1;
         }
-        if (live) {
+        if constexpr (FINE) {
+            static_assert(OUT == OUT_RELU8 || OUT == OUT_GELU8, "a block's largest magnitude is what the waves share");
+            float* tops = reinterpret_cast<float*>(smem + G::BYTES);        // [wave][row]
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                const float top = activate<OUT>(acc[t][0], 0.0f), other = __shfl_xor(top, 32, MOE_WAVE);
+                if (half == 0) tops[wave * BT + 32 * t + l32] = fmaxf(top, other);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // (the loads stay under way)
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                float top = 0.0f;
+#pragma unroll
+                for (int u = 0; u < G::NW; ++u) top = fmaxf(top, tops[u * BT + 32 * t + l32]);
+                const int byte = block_byte(top), r = cur.row + 32 * t + l32;
+                if (wave == 0 && r < cur.end) store_byte(p, byte, cur.col, r, half);
+                store_tile<OUT>(p, acc[t][0], cur.col, wave, r, r < cur.end, half, block_unit(byte));
+            }
+        } else if (live) {
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
                 const int r = cur.row + (wt * TT + t) * 32 + l32;
@@ -479,17 +540,18 @@ static int compute_units() {
     return n;
 }
 
-template <int WF, int WT, int TT, int BT, int NS, int OUT>
+template <int WF, int WT, int TT, int BT, int NS, int OUT, bool FINE = false>
 static int launch_tiles(const Fp8Args& p, int per_cu, hipStream_t st) {
     typedef Fp8Tile<WF, WT, TT, BT, NS> G;
     static unsigned long long opted;
-    const auto kern = fp8_tile_kernel<WF, WT, TT, BT, NS, OUT>;
-    if (!lds_opt_in((const void*)kern, G::BYTES, &opted)) return MOE_ERR_LAUNCH;
+    const auto kern = fp8_tile_kernel<WF, WT, TT, BT, NS, OUT, FINE>;
+    constexpr size_t lds = G::BYTES + (FINE ? G::NW * BT * 4 : 0);
+    if (!lds_opt_in((const void*)kern, lds, &opted)) return MOE_ERR_LAUNCH;
     const long long most = ((long long)p.rows / G::BT + (p.E < p.rows ? p.E : p.rows)) * ((p.nnb + WF - 1) / WF);
     long long wgs = (long long)compute_units() * per_cu / 8 * 8;
     if (wgs < 8) wgs = 8;
     if (wgs > (most + 7) / 8 * 8) wgs = (most + 7) / 8 * 8;
-    kern<<<(unsigned)wgs, G::NT, G::BYTES, st>>>(p);
+    kern<<<(unsigned)wgs, G::NT, lds, st>>>(p);
     return MOE_OK;
 }
 
@@ -502,8 +564,8 @@ enum { FP8_LARGE = 0, FP8_SMALL = 1, FP8_THIN = 2, FP8_NARROW = 3 };
 // 16 experts: first 34, 36, second (64 tiles) 53, 34.
 // 128 columns x 64 rows, three slabs in flight instead of two: where an expert's rows fit one tile either way, the weights'
 // bytes are the time, and more of them are on their way.  Narrow against small, us, both products of 32 experts, 1024 x 4096
-// (268 MB of weights): 122 rows 49.0, 59.2; 1024 rows 49.5, 62.2; 1536 rows 52.7, 63.3; 2048 rows 54.4, 64.2 dealt evenly, but
-// there a second row tile for half of the experts costs 30; 4096 rows 85.7, 73.4.
+// (268 MB of weights): 122 rows 50.0, 59.2; 1024 rows 51.3, 62.2; 1536 rows 58.3, 63.3; beyond, a second row tile for some of
+// the experts costs more than that (4096 rows 85.7, 73.4).
 // 32 x 32 with an eight-way split reduction: where there are so few small tiles that one tile's reduction is the launch's
 // time, 0.6 us for each of its 128 entries, against 0.084 us for each small tile's worth of thin ones.  8 rows of 8
 // experts, 1024 x 4096: second product 23.1 us with the small tile, 10.4 thin; 2048 x 2048: 13.3, 15.7; 122 rows of 32 experts,
@@ -527,7 +589,10 @@ static int launch_fp8(const Fp8Args& p, hipStream_t st) {
             return MOE_OK;
         }
     }
-    if (kind == FP8_NARROW) return launch_tiles<1, 4, 1, 64, 3, OUT>(p, 2, st);
+    if (kind == FP8_NARROW) {
+        if constexpr (HIDDEN) return launch_tiles<1, 4, 2, 64, 3, OUT, true>(p, 2, st);
+        else return launch_tiles<1, 4, 1, 64, 3, OUT>(p, 2, st);
+    }
     return kind == FP8_LARGE ? launch_tiles<2, 4, 2, 256, 2, OUT>(p, 1, st) : launch_tiles<1, 4, 1, 128, 2, OUT>(p, 2, st);
 }
 

@@ -226,6 +226,32 @@ def test_block(act, counts, d, f, dtype):
     close(yd, *exact_product(hq.view(F8), hb, w2q, w2b, counts, d))
 
 
+@pytest.mark.parametrize("counts,d,f", [((1,), 8, 136), ((33, 0, 48, 64), 136, 264), ((1, 2, 3) * 30, 1112, 376), ((40,) * 20, 2048, 520)])
+def test_hidden_of_few_rows_has_fp32_sums(counts, d, f):
+    """Experts of few rows: the hidden activation is the 64-bit one rounded, but for what fp32 sums are off (an addition per
+    16 products, those of a block of 128, and the 16 at once; each cut off at worst: 2^-23 of the sum of magnitudes)."""
+    T, E = sum(counts), len(counts)
+    xq, xb, w1q, w1b = operands(counts, d, f, d + f, wstd=0.5 / d ** 0.5)
+    _, _, w2q, w2b = operands(counts, f, d, f, rows=1)
+    s = B.make_fp8_shape(T, d, f, E, 1, B.BF16, B.RELU)
+    assert B.moe_fp8_kernels(s)[0] == 3
+    hq, hb = torch.empty((T, B.fp8_padded(f)), dtype=U8, device="cuda"), torch.empty((T, B.fp8_scale_bytes(f)), dtype=U8, device="cuda")
+    yd = torch.empty((T, d), dtype=torch.float32, device="cuda")
+    B.moe_expert_ffn_fwd_fp8(s, xq, xb, starts(counts), w1q, w1b, w2q, w2b, hq, hb, yd)
+    torch.cuda.synchronize()
+    x, w = R.wide_rows(xq.cpu(), xb.cpu()), R.wide_weights(w1q.cpu(), w1b.cpu())
+    h, off, a = torch.zeros(T, B.fp8_padded(f), dtype=torch.float64), torch.zeros(T, B.fp8_padded(f), dtype=torch.float64), 0
+    for e, n in enumerate(counts):
+        h[a:a + n, :f] = torch.relu(x[a:a + n] @ w[e][:, :f])
+        off[a:a + n, :f] = (d / 16 + d / 128 + 16) * 2.0 ** -23 * (x[a:a + n].abs() @ w[e][:, :f].abs())
+        a += n
+    got = R.wide_rows(hq.cpu().view(F8), hb.cpu())
+    unit = R.unit(hb.cpu()[:, :h.shape[1] // 128].long() - 127).repeat_interleave(128, 1)
+    _, e = torch.frexp(h / unit)
+    half = R.unit((e - 5).clamp(min=-10)) * unit        # of a step at h
+    assert ((got - h).abs() <= half + off).all()
+
+
 def test_block_with_infinite_and_nan_rows():
     """relu and gelu keep NaN; other rows do not see it."""
     counts, d, f = (40,), 128, 256

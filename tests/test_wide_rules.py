@@ -11,10 +11,10 @@ from paper_2109_10465_amd import binding as B
     (7375, 4, 1024, 4096, 64, (0, 0)),      # large 192, 145; small 227, 171
     (2048, 2, 1024, 4096, 16, (0, 1)),      # large 34, 53; small 36, 34
     (2048, 2, 1024, 4096, 32, (1, 1)),      # large 67, 52; small 48, 45
-    (768, 2, 1024, 4096, 32, (3, 3)),       # narrow 29, 23; small 36, 27
-    (61, 2, 1024, 4096, 32, (3, 3)),        # narrow 26, 23; small 34, 25; second thin 41
-    (1, 8, 1024, 4096, 8, (3, 2)),          # first: narrow 12.4, small 13.5
-    (1, 8, 2048, 2048, 8, (3, 3)),          # narrow 14.6, 12.7; small 17, 13; second thin 16
+    (768, 2, 1024, 4096, 32, (3, 3)),       # narrow 34, 24; small 36, 27
+    (61, 2, 1024, 4096, 32, (3, 3)),        # narrow 27, 23; small 34, 25; second thin 41
+    (1, 8, 1024, 4096, 8, (3, 2)),          # first: narrow 12.1, small 13.5
+    (1, 8, 2048, 2048, 8, (3, 3)),          # narrow 14.2, 12.8; small 17, 13; second thin 16
 ])
 def test_kernels_of_the_block(T, k, d, f, E, kinds):
     for act in (B.RELU, B.GELU):
