@@ -301,7 +301,11 @@ __device__ __forceinline__ Fp8Place fp8_place(const int* tiles, const int* start
 // rows: they are rounded to 4 bits, where a sum that is 2^-14 off falls to the other side of a tie in 1 of 900 entries, and
 // such steps of 6 % show where few rows are summed (48 rows of 376: outputs 0.3 % off, bf16's rounding 0.17).  The matrix
 // instructions take twice as long, which the weights' bytes hide.
-template <int WF, int WT, int TT, int BT, int NS, int OUT, bool FINE>
+// TURNS: the tiles begin their reduction at different slabs and come round.  Workgroups that walk rows of a multiple of 4096
+// bytes in step ask the same memory channels: second product of 122 rows, 32 experts, 1024 x 4096, weights from memory,
+// 34.3 us in step, 28.1 like this; with rows of 2048, 3968 or 4224 bytes 26 either way.  (Its instructions cost a token's
+// product 0.7 us: not where nothing is gained.)
+template <int WF, int WT, int TT, int BT, int NS, int OUT, bool FINE, bool TURNS>
 __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args p) {
     typedef Fp8Tile<WF, WT, TT, BT, NS> G;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -367,12 +371,15 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
     };
     // the cursor of the loads, NS - 1 slabs ahead of the products: the tile, its slab, and what is left of its operands
     Fp8Place next = fp8_place<G::BT, WF>(tiles, start, at, ctiles, lane);
-    int nkb = 0, group = 0;             // group: which buffer takes the exponents of the next four slabs
+    auto begin = [&](const Fp8Place& t) { return TURNS ? ((t.e * p.nnb + t.col) & 7) * 4 : 0; };
+    int nkb = begin(next), done = 0;    // the slab, and how many of the tile's went before
+    int group = 0;                      // which buffer takes the exponents of the next four slabs
     bool more = true;
     u32x4_buf_t wd, xd;
     auto aim = [&]() {
-        wd = desc((uint64_t)(p.wq + ((size_t)next.e * p.nnb + next.col) * 128 * kbytes), (uint64_t)(p.nnb - next.col) * 128 * kbytes);
-        xd = desc((uint64_t)(p.xq + (size_t)next.row * kbytes), (uint64_t)(next.end - next.row) * kbytes);
+        const uint32_t k = (uint32_t)nkb * 128;
+        wd = desc((uint64_t)(p.wq + ((size_t)next.e * p.nnb + next.col) * 128 * kbytes + k), (uint64_t)(p.nnb - next.col) * 128 * kbytes - k);
+        xd = desc((uint64_t)(p.xq + (size_t)next.row * kbytes + k), (uint64_t)(next.end - next.row) * kbytes - k);
     };
     auto step = [&](u32x4_buf_t& d) {   // 128 bytes further, and as much less to the end
         const uint32_t lo = d[0] + 128;
@@ -398,15 +405,23 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
         for (int i = 0; i < G::WL; ++i) load_to_lds(wd, voff[i], to + (i * G::NW + wave) * 1024);
 #pragma unroll
         for (int i = 0; i < G::XL; ++i) load_to_lds(xd, voff[i], to + G::BF * 128 + (i * G::NW + wave) * 1024);
-        if (++nkb < p.nkb) {
-            step(wd);
-            step(xd);
+        ++nkb;
+        if (++done < p.nkb) {
+            if (TURNS && nkb == p.nkb) {
+                nkb = 0;
+                if (more) aim();
+            } else {
+                step(wd);
+                step(xd);
+            }
         } else {
             nkb = 0;
+            done = 0;
             at += stride;
             more = more && at < total;
             if (more) {
                 next = fp8_place<G::BT, WF>(tiles, start, at, ctiles, lane);
+                nkb = begin(next);
                 aim();
             } else {
                 wd[2] = xd[2] = 0;
@@ -432,7 +447,8 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
         // a wave without rows (or columns) only helps to load: its products would cost the time of the others' and power, which
         // is what limits the clock
         const bool live = wt * TT * 32 < G::BT && cur.row + wt * TT * 32 < cur.end && cur.col + wf < p.nnb;
-        for (int kb = 0; kb < p.nkb; ++kb) {
+        int kb = begin(cur);
+        for (int n = 0; n < p.nkb; ++n) {
             // this slab has arrived once at most the NS - 2 younger ones are outstanding, and every wave is done with the one
             // before, whose place is filled again
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"((NS - 2) * (G::WL + G::XL)) : "memory");
@@ -493,6 +509,8 @@ __global__ __launch_bounds__(64 * WF * WT, 2) void fp8_tile_kernel(const Fp8Args
 #pragma unroll
             for (int t = 0; t < TT; ++t) xe[t] = (int)((uint32_t)xe[t] >> 8);
             stage = stage == NS - 1 ? 0 : stage + 1;
+            ++kb;
+            if (TURNS && kb == p.nkb) kb = 0;
         }
         if constexpr (FINE) {
             static_assert(OUT == OUT_RELU8 || OUT == OUT_GELU8, "a block's largest magnitude is what the waves share");
@@ -540,11 +558,11 @@ static int compute_units() {
     return n;
 }
 
-template <int WF, int WT, int TT, int BT, int NS, int OUT, bool FINE = false>
+template <int WF, int WT, int TT, int BT, int NS, int OUT, bool FINE = false, bool TURNS = false>
 static int launch_tiles(const Fp8Args& p, int per_cu, hipStream_t st) {
     typedef Fp8Tile<WF, WT, TT, BT, NS> G;
     static unsigned long long opted;
-    const auto kern = fp8_tile_kernel<WF, WT, TT, BT, NS, OUT, FINE>;
+    const auto kern = fp8_tile_kernel<WF, WT, TT, BT, NS, OUT, FINE, TURNS>;
     constexpr size_t lds = G::BYTES + (FINE ? G::NW * BT * 4 : 0);
     if (!lds_opt_in((const void*)kern, lds, &opted)) return MOE_ERR_LAUNCH;
     const long long most = ((long long)p.rows / G::BT + (p.E < p.rows ? p.E : p.rows)) * ((p.nnb + WF - 1) / WF);
@@ -590,8 +608,8 @@ static int launch_fp8(const Fp8Args& p, hipStream_t st) {
         }
     }
     if (kind == FP8_NARROW) {
-        if constexpr (HIDDEN) return launch_tiles<1, 4, 2, 64, 3, OUT, true>(p, 2, st);
-        else return launch_tiles<1, 4, 1, 64, 3, OUT>(p, 2, st);
+        constexpr int TT = HIDDEN ? 2 : 1;
+        return p.nkb % 32 ? launch_tiles<1, 4, TT, 64, 3, OUT, HIDDEN>(p, 2, st) : launch_tiles<1, 4, TT, 64, 3, OUT, HIDDEN, true>(p, 2, st);
     }
     return kind == FP8_LARGE ? launch_tiles<2, 4, 2, 256, 2, OUT>(p, 1, st) : launch_tiles<1, 4, 1, 128, 2, OUT>(p, 2, st);
 }

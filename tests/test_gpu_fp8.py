@@ -147,6 +147,34 @@ def test_larger_products(counts, K, N):
     close(y, want, off)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_of_4096_bytes(dtype):
+    """Many experts of few rows whose reductions begin at different places; data of any bytes, checked on the GPU."""
+    counts, K, N = (5, 0, 33, 64, 1, 2, 70) * 4, 4096, 1032
+    E, T, g = len(counts), sum(counts), torch.Generator(device="cuda").manual_seed(3)
+    assert B.moe_fp8_kernels(B.make_fp8_shape(T, N, K, E, 1, B.BF16, B.GELU))[1] == 3
+
+    def data(*shape):
+        v = torch.randint(0, 255, shape, generator=g, dtype=U8, device="cuda")
+        return torch.where((v & 0x7f) == 0x7f, 0, v).to(U8)
+
+    xq, wq = data(T, K), data(E, B.fp8_padded(N), K)
+    xb = torch.randint(118, 128, (T, K // 128), generator=g, dtype=U8, device="cuda")
+    wb = torch.randint(118, 128, (E, B.fp8_padded(N) // 128, K // 128), generator=g, dtype=U8, device="cuda")
+    y = torch.empty((T, N), dtype=dtype, device="cuda")
+    B.moe_expert_product_fp8(T, E, K, N, xq, xb, starts(counts), wq, wb, y)
+    torch.cuda.synchronize()
+    unit, a = lambda b: torch.exp2(b.double() - 127).repeat_interleave(128, -1), 0
+    for e, n in enumerate(counts):
+        x, w = xq[a:a + n].view(F8).double() * unit(xb[a:a + n]), wq[e].view(F8).double() * unit(wb[e]).repeat_interleave(128, 0)
+        w = w[:N].t().contiguous()
+        off = 7 * 2.0 ** -13 * (x.abs().reshape(n, K // 8, 8).amax(2) @ w.abs().reshape(K // 8, 8, N).amax(1)) if n else 0
+        off = off + K / 8 * 2.0 ** -23 * (x.abs() @ w.abs())
+        if n:
+            close(y[a:a + n], (x @ w).cpu(), off.cpu())
+        a += n
+
+
 def test_every_kernel_is_reached_above():
     kinds = lambda counts, d, f: B.moe_fp8_kernels(B.make_fp8_shape(sum(counts), d, f, len(counts), 1, B.BF16, B.GELU))
     assert kinds((2500, 1200, 0, 700), 264, 2056)[0] == 0 and kinds((900, 700, 800), 256, 512) == (1, 1)
@@ -226,7 +254,7 @@ def test_block(act, counts, d, f, dtype):
     close(yd, *exact_product(hq.view(F8), hb, w2q, w2b, counts, d))
 
 
-@pytest.mark.parametrize("counts,d,f", [((1,), 8, 136), ((33, 0, 48, 64), 136, 264), ((1, 2, 3) * 30, 1112, 376), ((40,) * 20, 2048, 520)])
+@pytest.mark.parametrize("counts,d,f", [((1,), 8, 136), ((33, 0, 48, 64), 136, 264), ((1, 2, 3) * 30, 1112, 376), ((40,) * 20, 2048, 520), ((9, 0, 40), 4096, 136)])
 def test_hidden_of_few_rows_has_fp32_sums(counts, d, f):
     """Experts of few rows: the hidden activation is the 64-bit one rounded, but for what fp32 sums are off (an addition per
     16 products, those of a block of 128, and the 16 at once; each cut off at worst: 2^-23 of the sum of magnitudes)."""
