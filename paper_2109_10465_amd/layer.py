@@ -125,20 +125,17 @@ class MoELayer:
         or bfloat16, contiguous) to the global norm max_norm, in place, and returns that norm (a device tensor of one float)."""
         if self.forward_only:
             raise B.MoeError("this layer was built forward-only")
+        others, dev = list(others), self.dWg.device
         for g in others:
-            if g.device != self.dWg.device:
-                raise B.MoeError(f"a gradient on {g.device}, not {self.dWg.device}")
+            if g.device != dev:
+                raise B.MoeError(f"a gradient on {g.device}, not {dev}")
         grads = B.make_grads([(g, g) for g in (self.dWg, self.dW1, self.dW2, *others)])
-        need = B.moe_grad_workspace_bytes(grads)
-        if self._clip is None or self._clip[1].numel() < need:
-            self._clip = (torch.empty(1, dtype=torch.float32, device=self.device),
-                          torch.empty(need, dtype=torch.uint8, device=self.device))
-        norm, ws = self._clip
-        with torch.cuda.device(self.device):
+        # of this call alone: a captured call keeps its own, whatever is clipped later
+        norm = torch.empty(1, dtype=torch.float32, device=dev)
+        ws = torch.empty(B.moe_grad_workspace_bytes(grads), dtype=torch.uint8, device=dev)
+        with torch.cuda.device(dev):
             B.moe_clip_grads(grads, max_norm, norm, ws)
         return norm
-
-    _clip = None        # norm and workspace of clip_gradients
 
 
 class Fp8MoELayer:
@@ -182,6 +179,7 @@ class Fp8MoELayer:
         self.hq, self.hb = buf((R, B.fp8_padded(d_ff)), u8), buf((R, B.fp8_scale_bytes(d_ff)), u8)
         self.yd, self.y = buf((R, d_model), torch.float32), buf((T, d_model), _TORCH_DT[dtype])
         self.ws = buf((nbytes,), u8)
+        self.device = self.y.device
         for t in (*W1, *W2):
             if t.device != self.y.device:
                 raise B.MoeError(f"8-bit weights on {t.device}, not {self.y.device}")

@@ -148,3 +148,18 @@ def test_a_layers_gradients_with_others():
     for g, s in zip(grads, src):
         tol = 2.0 ** -8 + 2.0 ** -21 if g.dtype == BF16 else 2.0 ** -21
         assert ((g.double() - 0.25 * s.double()).abs() <= tol * 0.25 * s.double().abs()).all()
+    # a captured call keeps what it works with: later calls have other norms, and more tensors
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = layer.clip_gradients(0.25 * want, [other])
+    big = [torch.full((300_000,), 1e-3, device="cuda") for _ in range(40)]
+    for again in range(3):
+        later = layer.clip_gradients(1e9, (b for b in big))
+        for g, s in zip(grads, src):
+            g.copy_(s)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert float(captured) == float(norm) and float(later) != float(norm)
+        assert (grads[1].double() - 0.25 * src[1].double()).abs().max() <= 2.0 ** -7 * src[1].double().abs().max()
+    with pytest.raises(B.MoeError):
+        layer.clip_gradients(1.0, [torch.zeros(4)])
