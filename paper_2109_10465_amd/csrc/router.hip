@@ -173,6 +173,8 @@ __global__ __launch_bounds__(256) void router_fwd_kernel(const RouterArgs a, con
             b[i] = BIAS && i < here ? bias[e0 + i] : 0.0f;
         }
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) l[i] = l[i] == l[i] ? l[i] : -INFINITY;     // a NaN would make the softmax's sum one
     // the softmax's largest logit and sum, where scores are compared or not divided by the chosen ones' sum
     const bool sums = a.n_groups > 1 && a.group_best == 2;
     float top = 0.0f, total = 1.0f;
@@ -197,7 +199,7 @@ __global__ __launch_bounds__(256) void router_fwd_kernel(const RouterArgs a, con
     for (int i = 0; i < 8; ++i) {
         float v = BIAS ? score(l[i]) + b[i] : l[i];
         v = __builtin_amdgcn_fmed3f(v, -2.9e38f, 2.9e38f);
-        v = l[i] > -INFINITY ? v : KEY_DEAD;        // (also NaN)
+        v = l[i] > -INFINITY ? v : KEY_DEAD;
         key[i] = __uint_as_float((__float_as_uint(v) & ~7u) | (uint32_t)i);
     }
     auto order = [&](int i, int j) {
@@ -308,8 +310,10 @@ __global__ __launch_bounds__(256) void router_bwd_kernel(const RouterArgs a, con
     if (dense) {
         if (in) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i) {
                 if (e4 + i < a.E) l[i] = row[e4 + i];
+                l[i] = l[i] == l[i] ? l[i] : -INFINITY;     // as the forward pass takes it
+            }
         }
         top = token_max<LPT>(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])));
         if (top == -INFINITY) top = 0.0f;
