@@ -407,11 +407,13 @@ typedef struct {
  *   With n_groups > 1, group g holds the E / n_groups consecutive experts from g * E / n_groups;
  *   its value is the largest v of its experts, or (group_best 2) the sum of the two largest
  *   s + select_bias.  Only experts of the top_groups groups of the largest values can be chosen.
+ *   Masked experts (a logit of -inf) have no part in it: a group with fewer than group_best others has
+ *   a value of -inf, and comes before one that has none.
  *   expert_idx[T,k] = the k experts with the largest v, best first
  *   gate_w[T,k]     = scale * s / (sum of the token's chosen s), or scale * s
  * Ties go to the smaller id, of groups and of experts.  The bias decides who is chosen and has
  * no part in the weights.  An expert whose logit is -inf (masked) scores 0 and is chosen only
- * where its token has no other; a NaN logit counts as -inf.  A logistic score below
+ * where its token's groups have no other; a NaN logit counts as -inf.  A logistic score below
  * 1e-299 (a logit below -690) counts as 0.  The weights of a token whose chosen scores are all
  * 0 are 0.  A chosen NaN gives its token undefined weights, a logit of +inf an undefined choice
  * too; never an index out of range.  Tokens with token_mask[t] == 0 (padding) get choices -1 and

@@ -38,6 +38,8 @@ template <typename V> __device__ __forceinline__ bool ahead(V va, int ia, V vb, 
 
 #define KEY_DEAD -3.0e38f       // an expert whose logit is -inf or NaN: after every other one (also without a finite value)
 #define KEY_OUT -3.3e38f        // one that cannot be chosen
+#define KEY_LEAST -2.9e38f      // the least of all others, and a group that has not as many experts as its value needs
+#define LEAST64 -1.7976931348623157e308     // the same among 64-bit values, where dead ones are -inf
 
 template <int CTRL> __device__ __forceinline__ float dpp(float v) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
@@ -92,7 +94,7 @@ __device__ __forceinline__ void choose64(const RouterArgs& a, const float* __res
         v[i] = l[i];
         if constexpr (BIAS) {
             const double w = score64(l[i], sigmoid, top, total) + (i < here ? (double)bias[e0 + i] : 0.0);
-            v[i] = l[i] > -INFINITY && w == w ? w : -INFINITY;
+            v[i] = l[i] > -INFINITY ? (w > LEAST64 ? w : LEAST64) : -INFINITY;      // (a bias of -inf does not make it a dead one)
         }
     }
     unsigned left = (1u << here) - 1u;          // experts that can still be chosen
@@ -114,7 +116,7 @@ __device__ __forceinline__ void choose64(const RouterArgs& a, const float* __res
             if constexpr (BIAS) gv = b0 + b1;
             else gv = b1 == -INFINITY ? -INFINITY : score64(b0, sigmoid, top, total) + score64(b1, sigmoid, top, total);
         }
-        if (!(gv == gv) || g >= a.n_groups) gv = -INFINITY;
+        if (b0 > -INFINITY && !(gv > LEAST64)) gv = LEAST64;    // one expert is more than none
         int before = 0;                         // groups in front of this one
         for (int o = 1; o < LPT >> a.lg_log2; ++o) {
             const double w = __shfl_xor(gv, o << a.lg_log2, MOE_WAVE);
@@ -198,7 +200,7 @@ __global__ __launch_bounds__(256) void router_fwd_kernel(const RouterArgs a, con
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         float v = BIAS ? score(l[i]) + b[i] : l[i];
-        v = __builtin_amdgcn_fmed3f(v, -2.9e38f, 2.9e38f);
+        v = __builtin_amdgcn_fmed3f(v, KEY_LEAST, -KEY_LEAST);
         v = l[i] > -INFINITY ? v : KEY_DEAD;
         key[i] = __uint_as_float((__float_as_uint(v) & ~7u) | (uint32_t)i);
     }
@@ -226,13 +228,14 @@ __global__ __launch_bounds__(256) void router_fwd_kernel(const RouterArgs a, con
             b0 = fmaxf(b0, c0);
         }
         float gv = b0;
-        if (a.group_best == 2) gv = b1 < -2.95e38f ? KEY_DEAD : BIAS ? b0 + b1 : score(b0) + score(b1);
+        const bool dead = b0 < -2.95e38f, whole = a.group_best == 1 ? !dead : !(b1 < -2.95e38f);
+        if (a.group_best == 2) gv = whole ? fmaxf(BIAS ? b0 + b1 : score(b0) + score(b1), KEY_LEAST) : dead ? KEY_DEAD : KEY_LEAST;
         if (g >= a.n_groups) gv = KEY_OUT;
         // A group's value is off by its keys' and scores' errors; where a score is made of a key, by that score's share of the
         // logit's (a softmax does not mind how large logits are, a key does).  The token's largest such error, twice, is near.
         float off = fmaf(fabsf(b0) + (a.group_best == 2 ? fabsf(b1) : 0.0f), 1.6e-6f, 1.6e-6f);
         if (!BIAS && a.group_best == 2) off = fmaf(fabsf(b0) + fabsf(b1), gv * 1.6e-6f, 1.6e-6f);
-        off = 2.0f * token_max<LPT>(gv < -2.95e38f ? 0.0f : off);
+        off = 2.0f * token_max<LPT>(whole ? off : 0.0f);
         int before = 0;
         for (int o = 1; o < LPT >> a.lg_log2; ++o) {
             const float w = __shfl_xor(gv, o << a.lg_log2, MOE_WAVE);
