@@ -35,20 +35,24 @@ __device__ __forceinline__ i32x8_t two16(uint4 a, uint4 b) {
     return i32x8_t{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
 }
 
-// gelu(z) = z Phi(z) with Phi(z) = 1 / (1 + 2^(-z P(z^2))): the logit of Phi is odd and smooth, and six coefficients of P,
-// fitted to 64 bits on |z| <= 5.5 with equal errors of gelu, leave 1.1e-6 of it (in fp32, over |z| <= 12).  A product
-// wide of the rounding to 8 bits, but an error e of a value moves a share e / step of the roundings, and their effect
-// on the output goes with the root of that: 1e-5 would be seen beside bfloat16's rounding.  18 instruction slots
-// (exponential and reciprocal four each) instead of the 33 of the two fits that the fp32 experts use: the epilogue of
-// the first product is bound by vector instructions.
+// gelu(z) = max(z, 0) - t Phi(-t) with t = |z|, and Phi(-t) = exp(-t^2 / 2) erfcx(t / sqrt 2) / 2, whose second factor is a
+// polynomial in u = 1 / (1 + 0.2975 t): seven coefficients, fitted to 64 bits on t <= 13.5 with equal relative errors, leave
+// 1.5e-6 of it.  So the error is a share of the value on the left too, where values fall to nothing: a block of 128 of
+// nothing but such values has an exponent of its own, and holds them as exactly as any other.  Below -13.2 the exponential is under
+// what fp32 holds, and gelu 0.  A 1.5e-6 is wide of the rounding to 8 bits, but an error e of a value moves a share e / step of
+// the roundings, and their effect on the output goes with the root of that: 1e-5 would be seen beside bfloat16's rounding.
+// 21 instruction slots (exponential and reciprocal four each) instead of the 33 of the two fits that the fp32 experts use: the
+// epilogue of the first product is bound by vector instructions.
 __device__ __forceinline__ float gelu(float z) {
-    constexpr float P[6] = {2.3021745681762695f, 0.10492697358131409f, -0.00016549293650314212f, -0.00013676212984137237f,
-                            8.115114724205341e-06f, -1.6478260533858702e-07f};
-    const float s = fminf(z * z, 30.25f);
-    float c = P[5];
+    constexpr float TAIL[7] = {-0.00011587030167f, 0.12084179371595f, 0.10217944532633f, 0.17530386149883f, -0.06812294572592f,
+                               0.25719109177589f, -0.08727779239416f};
+    constexpr float TAIL_AT = 0.2975f, LOG2E_HALF = -0.72134752044f;
+    const float t = __builtin_amdgcn_fmed3f(fabsf(z), 0.0f, 16.0f);    // (an infinite z: the tail is 0, not infinity times 0)
+    const float u = __builtin_amdgcn_rcpf(fmaf(TAIL_AT, t, 1.0f));
+    float r = TAIL[6];
 #pragma unroll
-    for (int i = 4; i >= 0; --i) c = fmaf(c, s, P[i]);
-    return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-z * c));
+    for (int i = 5; i >= 0; --i) r = fmaf(r, u, TAIL[i]);
+    return fmaf(-t, r * __builtin_amdgcn_exp2f(t * LOG2E_HALF * t), __builtin_elementwise_maximum(z, 0.0f));     // (keeps NaN)
 }
 
 // lanes 0..31 end with a = (own a, partner's a), lanes 32..63 with (partner's b, own b)
