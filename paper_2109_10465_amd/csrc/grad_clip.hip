@@ -99,46 +99,64 @@ __global__ __launch_bounds__(256) void grad_squares_kernel(const GradTable t, do
 }
 
 // the norm, in every thread of the workgroup
-__device__ __forceinline__ float norm_of(int n, const double* __restrict__ sums) {
+__device__ __forceinline__ double norm_of(int n, const double* sums) {
     double s = 0.0;
 #pragma unroll 8
     for (int i = threadIdx.x; i < n; i += 256) s += sums[i];
-    return (float)sqrt(block_sum(s));
+    return sqrt(block_sum(s));
 }
 
-__global__ __launch_bounds__(256) void grad_norm_kernel(int n, const double* __restrict__ sums, float* __restrict__ norm) {
-    const float v = norm_of(n, sums);
-    if (threadIdx.x == 0) norm[0] = v;
+// ... which also takes the first sum's place (every thread has read them)
+__global__ __launch_bounds__(256) void grad_norm_kernel(int n, double* sums, float* __restrict__ norm) {
+    const double v = norm_of(n, sums);
+    if (threadIdx.x == 0) {
+        norm[0] = (float)v;
+        sums[0] = v;
+    }
 }
+
+// The factor max_norm / norm as f 2^e: e is 0 but where the quotient is so small that fp32 would hold it with fewer bits, or as 0,
+// though its products with large gradients are not
+struct GradFactor {
+    float f;
+    int e;
+};
 
 template <typename T>
-__device__ __forceinline__ void scale_part(const T* p, T* o, int64_t a, int64_t b, float f) {
+__device__ __forceinline__ void scale_part(const T* p, T* o, int64_t a, int64_t b, GradFactor by) {
+    auto scaled = [by](float x) { return ldexpf(x * by.f, by.e); };
     if (((uintptr_t)p & 15) == ((uintptr_t)o & 15)) {
-        each_element<T>(p, a, b, [&](int64_t i, float x) { st_f32(o + i, x * f); },
+        each_element<T>(p, a, b, [&](int64_t i, float x) { st_f32(o + i, scaled(x)); },
                         [&](int64_t i, const float (&v)[Chunk<T>::N]) {
                             float w[Chunk<T>::N];
 #pragma unroll
-                            for (int j = 0; j < Chunk<T>::N; ++j) w[j] = v[j] * f;
+                            for (int j = 0; j < Chunk<T>::N; ++j) w[j] = scaled(v[j]);
                             Chunk<T>::store(o + i, w);
                         });
     } else {        // the output lies differently against 16 bytes
-        for (int64_t i = a + threadIdx.x; i < b; i += 256) st_f32(o + i, ld_f32(p + i) * f);
+        for (int64_t i = a + threadIdx.x; i < b; i += 256) st_f32(o + i, scaled(ld_f32(p + i)));
     }
 }
 
 __global__ __launch_bounds__(256) void grad_scale_kernel(const GradTable t, float max_norm, int n, const double* __restrict__ sums,
-                                                         float* norm) {
-    const float v = n ? norm_of(n, sums) : norm[0];
+                                                         float* __restrict__ norm) {
+    const double wide = n ? norm_of(n, sums) : sums[0];
+    const float v = (float)wide;
     if (n && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = v;  // (every launch writes the same)
     const bool clip = v > max_norm && v < INFINITY;
-    const float f = clip ? max_norm / v : 1.0f;
+    GradFactor by = {1.0f, 0};
+    if (clip) {
+        double q = max_norm / wide;
+        if (q < 0x1p-100) q = frexp(q, &by.e);
+        by.f = (float)q;
+    }
     for (int i = blockIdx.x; i < t.first[t.count]; i += gridDim.x) {
         const GradPart g = grad_part(t, i);
         const void* in = t.in[g.tensor];
         void* out = t.out[g.tensor];
         if (!clip && in == out) continue;
-        if (g.bf16) scale_part((const bf16_t*)in, (bf16_t*)out, g.begin, g.end, f);
-        else scale_part((const float*)in, (float*)out, g.begin, g.end, f);
+        if (g.bf16) scale_part((const bf16_t*)in, (bf16_t*)out, g.begin, g.end, by);
+        else scale_part((const float*)in, (float*)out, g.begin, g.end, by);
     }
 }
 
@@ -222,7 +240,7 @@ extern "C" int moe_grad_norm(const moe_grad* grads, int32_t count, float* norm, 
     if (!ws_ok(ws, ws_bytes, grad_ws_bytes(grads, count))) return MOE_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     const int n = squares_impl(grads, count, (double*)ws, st);
-    grad_norm_kernel<<<1, 256, 0, st>>>(n, (const double*)ws, norm);
+    grad_norm_kernel<<<1, 256, 0, st>>>(n, (double*)ws, norm);
     return launch_status();
 }
 
@@ -236,7 +254,7 @@ extern "C" int moe_clip_grads(const moe_grad* grads, int32_t count, float max_no
     hipStream_t st = (hipStream_t)stream;
     const int n = squares_impl(grads, count, (double*)ws, st);
     const bool apart = n == 0 || n > GRAD_SUMS;
-    if (apart) grad_norm_kernel<<<1, 256, 0, st>>>(n, (const double*)ws, norm);
+    if (apart) grad_norm_kernel<<<1, 256, 0, st>>>(n, (double*)ws, norm);
     each_table(grads, count, GRAD_CLIP_WGS, [&](const GradTable& t, int wgs) {
         grad_scale_kernel<<<wgs, 256, 0, st>>>(t, max_norm, apart ? 0 : n, (const double*)ws, norm);
     });
