@@ -159,8 +159,9 @@ class Fp8MoELayer:
             raise B.MoeError("unsupported router")
         for (q, b), (K, N) in ((W1, (d_model, d_ff)), (W2, (d_ff, d_model))):
             want = (E, B.fp8_padded(N), B.fp8_padded(K)), (E, B.fp8_padded(N) // 128, B.fp8_scale_bytes(K))
-            if (tuple(q.shape), tuple(b.shape)) != want or q.element_size() != 1 or b.dtype != torch.uint8:
-                raise B.MoeError(f"8-bit weights of shapes {want} expected, not {tuple(q.shape)}, {tuple(b.shape)}")
+            if (tuple(q.shape), tuple(b.shape)) != want or q.dtype not in (torch.float8_e4m3fn, torch.uint8) or b.dtype != torch.uint8:
+                raise B.MoeError(f"8-bit weights (float8_e4m3fn or its bytes, and uint8 exponents) of shapes {want} expected, not "
+                                 f"{q.dtype} of {tuple(q.shape)}, {b.dtype} of {tuple(b.shape)}")
             if not (q.is_contiguous() and b.is_contiguous()):
                 raise B.MoeError("8-bit weights must be contiguous")
         self.W1, self.W2 = W1, W2
