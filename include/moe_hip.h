@@ -413,9 +413,9 @@ typedef struct {
  *   gate_w[T,k]     = scale * s / (sum of the token's chosen s), or scale * s
  * Ties go to the smaller id, of groups and of experts.  The bias decides who is chosen and has
  * no part in the weights.  An expert whose logit is -inf (masked) scores 0 and is chosen only
- * where its token's groups have no other; a NaN logit counts as -inf.  A logistic score below
- * 1e-299 (a logit below -690) counts as 0.  The weights of a token whose chosen scores are all
- * 0 are 0.  A chosen NaN gives its token undefined weights, a logit of +inf an undefined choice
+ * where its token's groups have no other; a NaN logit counts as -inf.  In the
+ * weights, a logistic score below 1e-299 (a logit below -690) counts as 0; those of a token whose
+ * chosen scores are all 0 are 0.  A chosen NaN gives its token undefined weights, a logit of +inf an undefined choice
  * too; never an index out of range.  Tokens with token_mask[t] == 0 (padding) get choices -1 and
  * weights 0, and their logits are not read. */
 int moe_router_fwd(const moe_router* router, const float* logits, const float* select_bias_or_null,

@@ -252,10 +252,10 @@ __global__ __launch_bounds__(64 * THIN8_WAVES, 2) void fp8_thin_kernel(const Fp8
 // rows; NS slabs have a place in LDS, one is worked on, the others are being filled by loads that write LDS themselves.  A
 // workgroup walks its tiles and treats their slabs as one stream, so the next tile's first slabs are on their way during a
 // tile's epilogue.
-// Bound of the large tile, 131072 rows, 2048 x 8192, 16 experts: second product 1.80 ms (2440 TFLOP/s), where its matrix
+// Bound of the large tile, 131072 rows, 2048 x 8192, 16 experts: second product 1.82 ms (2420 TFLOP/s), where its matrix
 // instructions without the loads take 1.21 (3650 TFLOP/s: power holds the clock at 1.8 GHz of 2.4) and its loads without the
-// instructions 1.37 to 1.70, from the L2; 56 % of the matrix pipes' cycles are busy, no bank conflicts.  The first product, 2.40
-// with gelu and 2.00 with relu, adds its epilogue, which the one workgroup of a CU has nothing to overlap with but the
+// instructions 1.37 to 1.70, from the L2; 56 % of the matrix pipes' cycles are busy, no bank conflicts.  The first product, 2.47
+// with gelu and 2.03 with relu, adds its epilogue, which the one workgroup of a CU has nothing to overlap with but the
 // next tile's loads.  Neither fragments read ahead, a ring of four slabs of 64, nor loads that warm the L2 gained anything.
 template <int WF, int WT, int TT, int BT_, int NS_>
 struct Fp8Tile {
@@ -586,13 +586,14 @@ static int launch_tiles(const Fp8Args& p, int per_cu, hipStream_t st) {
 enum { FP8_LARGE = 0, FP8_SMALL = 1, FP8_THIN = 2, FP8_NARROW = 3 };
 // 256 x 256 or 128 x 128: a CU holds one workgroup of the large tile, which works off its area a fifth faster (half the
 // operands per product), or two of the small one; either way the launch takes whole rounds of tiles.  Measured, large against
-// small, us, first product with gelu and second: 131072 rows, 2048 x 8192, 16 experts: 2409, 2792 and 1775, 2226; 29500 rows,
-// 1024 x 4096, 64 experts: 205, 229 and 140, 171; 10006 rows, 776 x 3080, 6 experts with a Zipf gate: 58, 52 (three rounds
-// against four halves) and 43, 52; 4096 rows, 1024 x 4096, 16 experts: 28, 28 and (64 tiles) 51, 29.
+// small, us, first product with gelu, second with bf16 output, with fp32 output: 131072 rows, 2048 x 8192, 16 experts: 2470,
+// 2950; 1815, 2255; 1895, 2370.  29500 rows, 1024 x 4096, 64 experts: 207, 247; 140, 171; 152, 190.  10006 rows, 776 x 3080, 6
+// experts with a Zipf gate: 67, 54 (three rounds against four halves); 45, 53; 47, 55.  4096 rows, 1024 x 4096, 16 experts: 29,
+// 30; (64 tiles) 50, 30; 55, 31.
 // 128 columns x 64 rows, three slabs in flight instead of two: where an expert's rows fit one tile either way, the weights'
 // bytes are the time, and more of them are on their way.  Narrow against small, us, both products of 32 experts, 1024 x 4096
-// (268 MB of weights): 122 rows 50.0, 59.2; 1024 rows 51.3, 62.2; 1536 rows 58.3, 63.3; beyond, a second row tile for some of
-// the experts costs more than that (4096 rows 85.7, 73.4).
+// (268 MB of weights): 122 rows 51.7, 60.0; 1024 rows 52.4, 61.9; 1536 rows 59.4, 65.3; beyond, a second row tile for some of
+// the experts costs more than that (4096 rows 100, 77.6).
 // 32 x 32 with an eight-way split reduction: where there are so few tiles that one tile's reduction is the launch's
 // time, 0.6 us for each of its 128 entries, against 0.084 us for each tile's worth of thin ones.  Second products: 8 rows of
 // 8 experts, 1024 x 4096: 23.1 us with the small tile, 10.4 thin; 2048 x 2048: 12.8 with the narrow tile, 15.7 thin; 122 rows

@@ -16,11 +16,13 @@
 //
 // The choice is one of values in 64 bits.  It is made on keys of 32 bits, whose last three bits name the lane's entry:
 // a lane sorts its eight keys, and a round takes the largest head of the token's lanes, whose owner notes the expert
-// and moves on to its next key.  Where two values that matter - a choice and the next one, two groups - lie nearer
-// together than keys and fp32 scores can be off, the wave makes its choices again in 64 bits (about 1 in 100
-// tokens of 256 experts; equal logits always).  What bounds it is the number of vector instructions: 65536 tokens of 256
-// experts in 8 groups, top 8, take 48 us, 39 without groups and 31 without a bias too; all values in 64 bits took 190, and
-// the logits' read takes 14.
+// and moves on to its next key.  Where two values that matter - a choice and the next one, any two groups - lie nearer
+// together than keys and fp32 scores can be off, the wave makes its choices again in 64 bits.  With 256 experts that is about 1 in
+// 100 tokens of logistic scores in 8 groups, and more the more pairs of groups there are, most with softmax scores, whose sums
+// are small beside the errors allowed for; equal logits are always decided so, and tokens of two or more groups of masked
+// experts.  What bounds it is the number of vector instructions: 65536 tokens of 256 experts, top 8, 4 of 8 groups, take 49 us, 37
+// without groups and 30 without a bias too; the logits' read takes 14.  Softmax scores without a bias: 8 groups 46, 16 58, 32 93,
+// 64 284; two groups masked 118; all logits equal 116.
 struct RouterArgs {
     int T, E, k, score, n_groups, group, top_groups, group_best, renormalise;   // group = experts per group
     float scale;

@@ -13,7 +13,7 @@ def clean(l):
 
 def scores(row, sigmoid):
     if sigmoid:
-        return [1 / (1 + math.exp(-x)) if x > -690.0 else 0.0 for x in row]
+        return [1 / (1 + math.exp(-x)) if x > -709.0 else 0.0 for x in row]
     top = max(row)
     e = [math.exp(x - top) if x > -INF else 0.0 for x in row]
     total = sum(e)
