@@ -3,11 +3,11 @@
 // The list of tensors travels in the kernels' arguments, a table of them per launch.  A launch's tensors are cut into parts,
 // which its workgroups take in turn; each leaves one sum of squares, in 64 bits, in the workspace.  Up to 2048 of them
 // are added by every workgroup of the clipping launch itself, in one order: that is 16 KB of the L2 and saves a launch (157
-// tensors of 2.2 M elements together 15.7 us, 22.5 with it).  More of them, from a second table on, are added once: each launch would read them
-// for every part (300 tensors of 2^20 floats 247 us, 268 otherwise; 1200 tensors 986, 1453).  Squares are
+// tensors of 2.2 M elements together 15.5 us, 17.8 with it).  More of them, from a second table on, are added once: each launch would read them
+// for every part (300 tensors of 2^20 floats in place, not clipped, 248 us, 263 otherwise; 1200 tensors 976, 1436).  Squares are
 // summed in 64 bits because gradients may be anything that fp32 holds: the square of 2e19 is beyond fp32, that of 1e-23
-// below it.  Bound: HBM; everything is read twice and written once.  270 M floats and 130 M bfloat16: squares 254 us (5.3
-// TB/s), clipping 505 (5.3).  The clipping pass has a workgroup for nearly every part: with 2048 that take parts in turn it is
+// below it.  Bound: HBM; everything is read twice and written once.  270 M floats and 130 M bfloat16: squares 276 us (4.9
+// TB/s; 256 after a pause), clipping 497 (5.4).  The clipping pass has a workgroup for nearly every part: with 2048 that take parts in turn it is
 // 590 us; going backwards, from what the first pass read last, gains nothing.
 #include <math.h>
 #include "moe_common.h"
