@@ -5,6 +5,7 @@ memory; every call enqueues on torch's current stream unless `stream` is given.
 There is no fallback: if the library has not been built, importing a symbol
 raises.
 """
+import bisect
 import ctypes
 import os
 
@@ -499,7 +500,8 @@ def moe_fp8_kernels(shape):
 # ---- gradients of many tensors -------------------------------------------------------
 class Grads:
     """The list that moe_grad_norm and moe_clip_grads take: pairs (grad, out) of contiguous tensors of one type and
-    length; out may be grad itself, or None for the norm alone, and is no other pair's.  Keeps its tensors alive."""
+    length; out may be grad itself, or None for the norm alone, and shares no memory with anything else in the list.  Keeps its
+    tensors alive."""
 
     def __init__(self, pairs):
         self.pairs = [tuple(p) for p in pairs]
@@ -511,9 +513,19 @@ class Grads:
                 if t.dtype != g.dtype or t.numel() != g.numel():
                     raise MoeError("a gradient and its output must agree in type and length")
             m.grad, m.out, m.n, m.dtype = _p(g), _p(o), g.numel(), _dtype_of(g)
-        outs = [_p(o) for _, o in self.pairs if o is not None and o.numel()]
-        if len(set(outs)) != len(outs):
-            raise MoeError("an output is in the list twice")
+        span = lambda t: (_p(t), _p(t) + t.numel() * t.element_size())
+        outs = sorted(span(o) for _, o in self.pairs if o is not None and o.numel())
+        if any(a[1] > b[0] for a, b in zip(outs, outs[1:])):
+            raise MoeError("an output is in the list twice, or overlaps another one")
+        if outs:
+            starts = [a for a, _ in outs]
+            for g, o in self.pairs:
+                if not g.numel() or (o is not None and _p(o) == _p(g)):
+                    continue        # (in place: it is one of the outputs)
+                a, b = span(g)
+                at = bisect.bisect_left(starts, b) - 1      # the last output that starts before the gradient's end
+                if at >= 0 and outs[at][1] > a:
+                    raise MoeError("an output overlaps a gradient")
 
 
 def make_grads(pairs):
