@@ -491,8 +491,8 @@ int moe_dispatch_fp8(const moe_fp8_shape* shape, const void* x, const int32_t* r
                      uint8_t* xb, void* stream);
 
 /* The experts' block: h = act(x W1) in 8 bits -> hq[R,Kp(d_ff)], hb;  yd[R,d_model] = h W2, of type
- * yd_dtype.  The hidden activation is formed in fp32 (gelu is 4e-7 off at most, and for negative
- * arguments 1e-5 of its value; below -12.9 it may be 0) and rounded once, to the format
+ * yd_dtype.  The hidden activation is formed in fp32 (gelu within 4e-7 before its own rounding, for
+ * negative arguments within 2e-5 of its value; below -12.9 it may be 0) and rounded once, to the format
  * above (with exponents not below -126, and NaN passed over in finding them).  With at most 48 rows per
  * expert on average its sums are as exact as fp32's: a sum that falls to the other side of a rounding
  * moves an entry by 6 %, which shows where few rows are all there is. */

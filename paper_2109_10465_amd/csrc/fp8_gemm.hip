@@ -39,7 +39,7 @@ __device__ __forceinline__ i32x8_t two16(uint4 a, uint4 b) {
 // polynomial in u = 1 / (1 + 0.2975 t): seven coefficients, fitted to 64 bits on t <= 13.5 with equal relative errors, leave
 // 1.5e-6 of it.  So the error is a share of the value on the left too, where values fall to nothing: a block of 128 of
 // nothing but such values has an exponent of its own, and holds them as exactly as any other.  Below -13.2 the exponential is under
-// what fp32 holds, and gelu 0.  A 1.5e-6 is wide of the rounding to 8 bits, but an error e of a value moves a share e / step of
+// what fp32 holds, and gelu 0.  Rounded to 8 bits, less would do, but an error e of a value moves a share e / step of
 // the roundings, and their effect on the output goes with the root of that: 1e-5 would be seen beside bfloat16's rounding.
 // 21 instruction slots (exponential and reciprocal four each) instead of the 33 of the two fits that the fp32 experts use: the
 // epilogue of the first product is bound by vector instructions.
